@@ -549,6 +549,59 @@ int32_t pf_op_gemm_tn(int32_t dtype, const void* A, const void* B, float* C, flo
 int32_t pf_op_embed(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, void* x,
                     int64_t tokens, int32_t S, int32_t d, int32_t V, void* stream);
 
+/* ---- packed sequences -------------------------------------------------------------------------------------------
+ * A batch whose sequences have different lengths and lie one behind the other, without padding, in the rows of one
+ * buffer of `tokens` rows.  seq_start (device int32 [n_seq + 1], ascending): sequence s is rows seq_start[s] ..
+ * seq_start[s + 1] - 1, empty ones are allowed; NULL with n_seq 0: all rows are one sequence.  Rows before the first
+ * or behind the last sequence (a buffer of fixed size that is not full) are in none: results are not written there
+ * (they keep what they hold) and these rows contribute to nothing, whatever they hold.  seq_start stays on the device, so a captured
+ * graph can be replayed with other lengths in the same buffers; the host cannot check it.  Values out of order or out
+ * of range leave the results undefined, but nothing is read or written outside the buffers.
+ * These calls allocate nothing, keep nothing between calls and give the same results every time (no atomics on
+ * results).  Buffers, workspace and stream belong to the current device; calls that overlap in time (other streams,
+ * captured graphs replayed side by side) need workspaces and results of their own.  Results must not overlap operands. */
+typedef struct pf_packed_attn {
+  int64_t tokens;              /* rows of every operand                                                              */
+  int64_t ld_q, ld_k, ld_v;    /* elements between rows of q, k, v (and of dq, dk, dv); 0: rows without gaps          */
+  int64_t ld_out;              /* the same for out and dout                                                           */
+  int32_t n_seq;
+  int32_t dtype;               /* PF_DTYPE_*: storage type of all operands and gradients                              */
+  int32_t n_heads;             /* heads of q and out                                                                  */
+  int32_t n_kv_heads;          /* heads of k and v, a divisor of n_heads: head i reads K/V head i / (n_heads / n_kv_heads) */
+  int32_t d_head;              /* 8, 16, 32, 64 or 128                                                                */
+  int32_t causal;              /* != 0: a row sees the rows of its sequence up to itself; 0: its whole sequence        */
+} pf_packed_attn;
+/* out = softmax(Q K^T / sqrt(d_head)) V within each sequence.  Row t of q: n_heads * d_head elements from q + t * ld_q
+ * (k, v: n_kv_heads * d_head), so q, k, v may be column blocks of one fused projection.  lse (fp32
+ * [n_heads][tokens], may be NULL): log-sum-exp of the scaled scores, for the backward pass.  Infinities and NaN in
+ * rows that a query does not see do not reach its result.  tokens * n_heads at most 2^27.  Fastest with 16-byte
+ * aligned pointers and strides in eights; any alignment to whole elements is accepted. */
+int32_t pf_op_attention_packed(const pf_packed_attn* desc, const int32_t* seq_start, const void* q, const void* k,
+                               const void* v, void* out, float* lse, void* stream);
+/* Bytes of workspace pf_op_attention_packed_bwd needs (<0: error code); a function of desc alone. */
+int64_t pf_op_attention_packed_bwd_workspace(const pf_packed_attn* desc);
+/* Gradients from the saved out and lse: dq, dk, dv with the layout and strides of q, k, v, overwritten; dk and dv are
+ * summed over the query heads that share them, in fp32.  workspace: device, 256-byte aligned; PF_ERR_NOMEM if
+ * workspace_bytes is too small. */
+int32_t pf_op_attention_packed_bwd(const pf_packed_attn* desc, const int32_t* seq_start, const void* q, const void* k,
+                                   const void* v, const void* out, const void* dout, const float* lse, void* dq,
+                                   void* dk, void* dv, void* workspace, int64_t workspace_bytes, void* stream);
+/* x[t] = scale * tok[ids[t]] + pos[t - start of its sequence], rounded once.  ids: int32 [tokens]; tok [V][d]; pos
+ * [S][d], or NULL: no position term.  ids outside [0,V) and positions from S on contribute zeros.  d a multiple of 8;
+ * tok, pos and x 16-byte aligned; V and S at most 2^24, tokens * ceil(d / 512) at most 2^26. */
+int32_t pf_op_embed_packed(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, const int32_t* seq_start,
+                           int32_t n_seq, float scale, void* x, int64_t tokens, int32_t S, int32_t d, int32_t V,
+                           void* stream);
+/* Bytes of workspace pf_op_embed_packed_bwd needs (<0: error code). */
+int64_t pf_op_embed_packed_bwd_workspace(int64_t tokens, int32_t S, int32_t d, int32_t V);
+/* Gradients of pf_op_embed_packed by sorted tokens: dtok[v] = scale * sum over rows t with ids[t] = v of dx[t] (fp32
+ * [V][d]), dpos[p] = sum over rows at position p of dx[t] (fp32 [S][d], may be NULL).  dx: [tokens][d] of dtype.
+ * accumulate == 0: both are overwritten as a whole, with zeros where no row contributes; else added to.  Rows are added
+ * in a fixed order, in fp32.  workspace: device, 256-byte aligned; PF_ERR_NOMEM if workspace_bytes is too small. */
+int32_t pf_op_embed_packed_bwd(int32_t dtype, const void* dx, const int32_t* ids, const int32_t* seq_start, int32_t n_seq,
+                               float scale, float* dtok, float* dpos, int32_t accumulate, void* workspace,
+                               int64_t workspace_bytes, int64_t tokens, int32_t S, int32_t d, int32_t V, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,8 @@ EXPORTS = [
     "pf_ctx_set_replan", "pf_main_opt_state_bytes", "pf_ctx_set_main_offload", "pf_ctx_kernel_timing_every", "pf_ctx_train_state", "pf_ctx_read_params", "pf_op_gemm", "pf_op_layernorm", "pf_op_attention",
     "pf_op_embed", "pf_ctx_kernel_timing", "pf_ctx_kernel_stats", "pf_op_attention_bwd", "pf_op_layernorm_bwd", "pf_op_transpose", "pf_op_gemm_tn",
     "pf_op_layernorm_bwd_static", "pf_select_config_stream", "pf_main_stage_read", "pf_probe_bubbles_live",
+    "pf_op_attention_packed", "pf_op_attention_packed_bwd", "pf_op_attention_packed_bwd_workspace", "pf_op_embed_packed",
+    "pf_op_embed_packed_bwd", "pf_op_embed_packed_bwd_workspace",
 ]
 PF_K_GEMM_QKV, PF_K_GEMM_OUT, PF_K_GEMM_FFN1, PF_K_GEMM_FFN2, PF_K_ATTENTION, PF_K_LAYERNORM, PF_K_EMBED, PF_K_COPY_WAIT = range(8)
 
@@ -88,6 +90,12 @@ class pf_weights(C.Structure):
 class pf_adam(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("accum", C.c_int32)]
+
+
+class pf_packed_attn(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_out", C.c_int64),
+                ("n_seq", C.c_int32), ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("d_head", C.c_int32), ("causal", C.c_int32)]
 
 
 class pf_timeline_stats(C.Structure):
@@ -157,6 +165,14 @@ def _load():
     lib.pf_op_transpose.argtypes = [I32, VP, VP, I64, I64, VP, VP]
     lib.pf_op_gemm_tn.argtypes = [I32, VP, VP, VP, VP, I64, I64, I64, VP]
     lib.pf_op_embed.argtypes = [I32, VP, VP, VP, VP, I64, I32, I32, I32, VP]
+    lib.pf_op_attention_packed.argtypes = [P(pf_packed_attn), VP, VP, VP, VP, VP, VP, VP]
+    lib.pf_op_attention_packed_bwd_workspace.argtypes = [P(pf_packed_attn)]
+    lib.pf_op_attention_packed_bwd_workspace.restype = I64
+    lib.pf_op_attention_packed_bwd.argtypes = [P(pf_packed_attn)] + [VP] * 11 + [I64, VP]
+    lib.pf_op_embed_packed.argtypes = [I32, VP, VP, VP, VP, I32, C.c_float, VP, I64, I32, I32, I32, VP]
+    lib.pf_op_embed_packed_bwd_workspace.argtypes = [I64, I32, I32, I32]
+    lib.pf_op_embed_packed_bwd_workspace.restype = I64
+    lib.pf_op_embed_packed_bwd.argtypes = [I32, VP, VP, VP, I32, C.c_float, VP, VP, I32, VP, I64, I64, I32, I32, I32, VP]
     return lib
 
 
@@ -587,3 +603,42 @@ def pf_op_transpose(dtype, src, dst, rows, cols, colsum_acc=None, stream=None):
 
 def pf_op_attention_bwd(dtype, qkv, out, dout, lse, dsum, dqkv, B, S, h, dh, causal, stream=None):
     _check(lib.pf_op_attention_bwd(dtype, qkv, out, dout, lse, dsum, dqkv, B, S, h, dh, int(bool(causal)), stream))
+
+
+# ------------------------------------------------------------------------------------------ packed sequences
+def packed_attn(dtype, tokens, n_seq, n_heads, n_kv_heads, d_head, causal, ld_q=0, ld_k=0, ld_v=0, ld_out=0):
+    """Description of a packed attention call; strides in elements, 0: rows without gaps."""
+    return pf_packed_attn(tokens, ld_q, ld_k, ld_v, ld_out, n_seq, dtype, n_heads, n_kv_heads, d_head, int(bool(causal)))
+
+
+def pf_op_attention_packed(desc, seq_start, q, k, v, out, lse=None, stream=None):
+    _check(lib.pf_op_attention_packed(C.byref(desc), seq_start, q, k, v, out, lse, stream))
+
+
+def pf_op_attention_packed_bwd_workspace(desc):
+    n = lib.pf_op_attention_packed_bwd_workspace(C.byref(desc))
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def pf_op_attention_packed_bwd(desc, seq_start, q, k, v, out, dout, lse, dq, dk, dv, workspace, workspace_bytes, stream=None):
+    _check(lib.pf_op_attention_packed_bwd(C.byref(desc), seq_start, q, k, v, out, dout, lse, dq, dk, dv, workspace,
+                                          workspace_bytes, stream))
+
+
+def pf_op_embed_packed(dtype, ids, tok, pos, seq_start, n_seq, scale, x, tokens, S, d, V, stream=None):
+    _check(lib.pf_op_embed_packed(dtype, ids, tok, pos, seq_start, n_seq, scale, x, tokens, S, d, V, stream))
+
+
+def pf_op_embed_packed_bwd_workspace(tokens, S, d, V):
+    n = lib.pf_op_embed_packed_bwd_workspace(tokens, S, d, V)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def pf_op_embed_packed_bwd(dtype, dx, ids, seq_start, n_seq, scale, dtok, dpos, accumulate, workspace, workspace_bytes,
+                           tokens, S, d, V, stream=None):
+    _check(lib.pf_op_embed_packed_bwd(dtype, dx, ids, seq_start, n_seq, scale, dtok, dpos, int(bool(accumulate)), workspace,
+                                      workspace_bytes, tokens, S, d, V, stream))

@@ -71,6 +71,26 @@ hipError_t attention_fwd(int32_t dtype, const void* qkv, void* out, float* lse, 
 hipError_t embed_fwd(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, void* x,
                      int64_t tokens, int32_t S, int32_t d, int32_t V, hipStream_t stream);
 
+// ---- packed sequences: different lengths, one behind the other ----------------------------------------
+// seq_start: device int32 [n_seq + 1], or null with n_seq 0 (all rows are one sequence).  Rows in no sequence are not written
+// and contribute to nothing.
+struct PackedAttn {
+  int64_t tokens, ld_q, ld_k, ld_v, ld_out;   // rows, and elements between them; gradients lie as their operands
+  const int32_t* seq_start;
+  int32_t n_seq, dtype, h, h_kv, dh, causal;
+};
+hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse,
+                                hipStream_t stream);
+int64_t attention_packed_bwd_bytes(const PackedAttn& a);   // of workspace
+hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* out, const void* dout,
+                                const float* lse, void* dq, void* dk, void* dv, void* workspace, hipStream_t stream);
+hipError_t embed_packed_fwd(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, const int32_t* seq_start,
+                            int32_t n_seq, float scale, void* x, int64_t tokens, int32_t S, int32_t d, int32_t V, hipStream_t stream);
+int64_t embed_packed_bwd_bytes(int64_t tokens, int32_t S, int32_t d, int32_t V);
+hipError_t embed_packed_bwd(int32_t dtype, const void* dx, const int32_t* ids, const int32_t* seq_start, int32_t n_seq, float scale,
+                            float* dtok, float* dpos, int32_t accumulate, void* workspace, int64_t tokens, int32_t S, int32_t d,
+                            int32_t V, hipStream_t stream);
+
 // ---- training-only kernels -----------------------------------------------------------------------------
 // out[c][r] = in[r][c]
 hipError_t transpose2d(int32_t dtype, const void* in, void* out, int64_t R, int64_t C, hipStream_t stream);
