@@ -8,7 +8,8 @@ result (2^-8 of it), and the bf16 products (d_head 64 and 128) round P and dS (2
   dv    (r + fp) sum P |do|                                      + 2^-8 |dv|
   dq    scale sum ((r + fp) |dS| + P e) |k|, dk the same with |q| + 2^-8 of each,
         e = 2^-24 (dh + 2) (|do| |v| + |do| |out|) the error of dP - D
-with r = 2^-8 or 0."""
+with r = 2^-8 or 0.  A probability below 2^-126 may become 0: of at most 2^12 terms each, with factors |dP - D| |q| up to 2^19
+(2 * 128 * 4.5^2 and 16 * 4.5), that is 2^-95 more."""
 import numpy as np
 import pytest
 
@@ -19,7 +20,7 @@ torch = pytest.importorskip("torch")
 from oracle import packed as opk          # noqa: E402
 from paper_2410_07192_amd import synth    # noqa: E402
 
-U32, U16 = 2.0 ** -24, 2.0 ** -8
+U32, U16, FLUSHED = 2.0 ** -24, 2.0 ** -8, 2.0 ** -95
 
 
 def _mods():
@@ -44,6 +45,8 @@ class Case:
         self.live[first:self.start[-1]] = True
         if edit:
             edit(self)
+            if dtype == "bf16":      # what the device gets: the checker has to start from the same numbers
+                self.q, self.k, self.v, self.do = (torch.from_numpy(x).to(torch.bfloat16).float().numpy() for x in (self.q, self.k, self.v, self.do))
         for x in (self.q, self.k, self.v, self.do):
             x[~self.live] = np.nan
         self.shift = shift
@@ -103,7 +106,9 @@ class Case:
         stored = U16 if self.dtype == "bf16" else U32
         return stored, (U16 if self.dtype == "bf16" and self.dh in (64, 128) else 0.0)
 
-    def check_forward(self, got=None):
+    def check_forward(self, got=None, rows=None):
+        """rows: the ones that are compared (default: all that are in a sequence)."""
+        rows = self.live if rows is None else rows & self.live
         q, k, v, _ = self.wide()
         out, lse = opk.attention(q, k, v, self.start, self.causal)
         o, L = got or self.forward()
@@ -116,9 +121,11 @@ class Case:
                 top = (np.abs(q[a:b, i]) @ np.abs(ka).T).max() / np.sqrt(self.dh)
                 fp = U32 * ((self.dh + 4) * top + n + 16)
                 p = np.exp(opk.scores(q[a:b, i], ka, self.causal) - lse[i, a:b, None])
-                tol = (r + 2 * fp) * (p @ va) + stored * np.abs(out[a:b, i])
-                assert (np.abs(o[a:b, i] - out[a:b, i]) <= tol).all(), (a, b, i, np.abs((o[a:b, i] - out[a:b, i]) / tol).max())
-                assert (np.abs(L[i, a:b] - lse[i, a:b]) <= fp + 4 * U32 * np.abs(lse[i, a:b])).all(), (a, b, i)
+                tol = (r + 2 * fp) * (p @ va) + stored * np.abs(out[a:b, i]) + FLUSHED
+                r_ = rows[a:b]
+                err = np.abs(o[a:b, i] - out[a:b, i])[r_]
+                assert (err <= tol[r_]).all(), (a, b, i, (err / tol[r_]).max())
+                assert (np.abs(L[i, a:b] - lse[i, a:b]) <= fp + 4 * U32 * np.abs(lse[i, a:b]))[r_].all(), (a, b, i)
         return o, L
 
     def saved(self):
@@ -127,7 +134,8 @@ class Case:
         out = out.astype(np.float32)
         return (synth.round_to_bf16(out) if self.dtype == "bf16" else out).reshape(out.shape), lse.astype(np.float32)
 
-    def check_backward(self, got=None):
+    def check_backward(self, got=None, rows=None):
+        rows = self.live if rows is None else rows & self.live
         q, k, v, do = self.wide()
         out, lse = self.saved()
         got = got or self.backward(out, lse)
@@ -135,7 +143,7 @@ class Case:
         want = opk.attention_backward(q, k, v, out, do, lse, self.start, self.causal)
         stored, r = self.rounding()
         g, scale = self.h // self.kv, 1 / np.sqrt(self.dh)
-        tol = [stored * np.abs(w) for w in want]
+        tol = [stored * np.abs(w) + FLUSHED for w in want]
         for a, b in opk.spans(self.start):
             n = b - a
             for i in range(self.h):
@@ -151,8 +159,8 @@ class Case:
                 tol[1][a:b, j] += scale * (w.T @ np.abs(qi))
                 tol[2][a:b, j] += (r + fp) * (p.T @ np.abs(di))
         for name, x, w, t in zip(("dq", "dk", "dv"), got, want, tol):
-            bad = np.abs(x - w)[self.live] > t[self.live]
-            assert not bad.any(), (name, int(bad.sum()), np.abs((x - w)[self.live] / np.maximum(t[self.live], 1e-30)).max())
+            bad = ~(np.abs(x - w)[rows] <= t[rows])
+            assert not bad.any(), (name, int(bad.sum()), np.abs((x - w)[rows] / np.maximum(t[rows], 1e-30)).max())
         return got
 
 
@@ -214,7 +222,7 @@ def test_one_sequence_without_boundaries():
 @pytest.mark.parametrize("dtype,h,kv,dh", [("bf16", 4, 2, 64), ("bf16", 8, 1, 128), ("bf16", 2, 2, 32), ("f32", 4, 2, 64)])
 @pytest.mark.parametrize("causal", [False, True])
 def test_values_that_a_row_does_not_see_do_not_reach_it(dtype, h, kv, dh, causal):
-    """Infinities and NaN in one sequence (and, causal, in the last rows of another) leave the rest as it is without them."""
+    """Infinities and NaN in one sequence (and, causal, in the last rows of another) leave the rest as it would be without them."""
     lens = [70, 45, 20, 130, 9]
 
     def poison(c):
@@ -234,11 +242,9 @@ def test_values_that_a_row_does_not_see_do_not_reach_it(dtype, h, kv, dh, causal
     late = clean.copy()
     if causal:
         late[good.start[4] - 6:good.start[4]] = False
-    (o0, l0), (o1, l1) = good.check_forward(), bad.forward()
-    assert np.array_equal(o0[late & good.live], o1[late & good.live]) and np.array_equal(l0[:, late & good.live], l1[:, late & good.live])
-    assert np.isnan(o1[good.start[1]:good.start[2]]).any()
+    o, _ = good.check_forward(bad.forward(), late)      # the checker's values without them, to the same tolerance
+    assert np.isnan(o[good.start[1]:good.start[2]]).any()
     out, lse = good.saved()
-    g0 = good.check_backward()
 
     def poison_qd(c):   # the backward pass: other sequences' rows, and rows of this one that come before (causal queries)
         poison_all = slice(c.start[1], c.start[2])
@@ -250,12 +256,10 @@ def test_values_that_a_row_does_not_see_do_not_reach_it(dtype, h, kv, dh, causal
                 x[c.start[3]:c.start[3] + 5] = np.nan
 
     bad = Case(dtype, lens, h, kv, dh, causal, 1, 2, seed=3, edit=poison_qd)
-    g1 = bad.backward(out, lse)
-    keys = clean & good.live
+    keys = clean.copy()
     if causal:
         keys[good.start[3]:good.start[3] + 5] = False
-    assert np.array_equal(g0[0][keys], g1[0][keys])
-    assert np.array_equal(g0[1][keys], g1[1][keys]) and np.array_equal(g0[2][keys], g1[2][keys])
+    good.check_backward(bad.backward(out, lse), keys)
 
 
 @pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("f32", 64)])
