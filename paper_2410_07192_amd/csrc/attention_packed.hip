@@ -402,6 +402,9 @@ bool aligned16(const PackedAttn& a, std::initializer_list<const void*> ptrs) {
   return a.ld_q % 8 == 0 && a.ld_k % 8 == 0 && a.ld_v % 8 == 0 && a.ld_out % 8 == 0;
 }
 
+// whether bf16 products are used: they round P and dS, as the storage type rounds the results, and are 16 times as fast
+bool by_bf16(const PackedAttn& a) { return a.dtype == PF_DTYPE_BF16_ && (a.dh == 64 || a.dh == 128); }
+
 template <typename T, int DH, bool VEC>
 hipError_t fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
   const unsigned grid = (unsigned)((a.tokens + 31) / 32 * a.h);
@@ -438,6 +441,7 @@ hipError_t bwd(const PackedAttn& a, const void* q, const void* k, const void* v,
 
 hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
   const bool vec = aligned16(a, {q, k, v, out});
+  if (vec && by_bf16(a)) return packed_fwd_bf16(a, operands<bf16_t>(a, q, k, v), out, lse, st);
 #define PF_FWD(T, D, V) fwd<T, D, V>(a, q, k, v, out, lse, st)
   PF_BY_SHAPE(PF_FWD);
 #undef PF_FWD
