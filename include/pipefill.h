@@ -562,7 +562,7 @@ int32_t pf_op_embed(int32_t dtype, const int32_t* ids, const void* tok, const vo
  * captured graphs replayed side by side) need workspaces and results of their own.  Results must not overlap operands. */
 typedef struct pf_packed_attn {
   int64_t tokens;              /* rows of every operand                                                              */
-  int64_t ld_q, ld_k, ld_v;    /* elements between rows of q, k, v (and of dq, dk, dv); 0: rows without gaps          */
+  int64_t ld_q, ld_k, ld_v;    /* elements between rows of q, k, v (and of dq, dk, dv), at most 2^24; 0: no gaps      */
   int64_t ld_out;              /* the same for out and dout                                                           */
   int32_t n_seq;
   int32_t dtype;               /* PF_DTYPE_*: storage type of all operands and gradients                              */

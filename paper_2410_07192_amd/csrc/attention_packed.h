@@ -32,6 +32,45 @@ __device__ __forceinline__ Span queries_of(const PackedRows& p, int r0, int row,
 // value of lane `lane`, as a scalar
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
+// sum over the wave, the same in all lanes
+__device__ __forceinline__ int wave_total(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: lane 15 of each row has its sum
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  return lane_value(x, 15) + lane_value(x, 31) + lane_value(x, 47) + lane_value(x, 63);
+}
+
+// Which of `blocks` blocks of 2^log_rows rows the i-th workgroup takes: those that meet most rows first, so that none of them is
+// the last to start.  n_s blocks begin in sequence s.  Causal, the j-th of them meets j blocks' rows (from_end: of keys that
+// queries see, counted from the sequence's end), so block i is the one at depth X, the largest with sum over s of max(0, n_s - X) > i;
+// not causal, all n_s of them meet n_s blocks' rows.  (Only where not all workgroups start at once: it takes a microsecond.)  For up to 64 sequences, one a lane; more (short ones, mostly) are taken from the end on.
+__device__ __forceinline__ int block_in_order(const PackedRows& p, int i, int blocks, int log_rows, int causal, bool from_end, bool at_once) {
+  const int plain = causal && from_end ? i : blocks - 1 - i;
+  if (at_once || p.start == nullptr || p.n_seq < 2 || p.n_seq > 64) return plain;
+  const int lane = threadIdx.x & 63, up = (1 << log_rows) - 1;
+  int b0 = 0, n = 0;
+  if (lane < p.n_seq) {   // rows before the first sequence count as its own, rows behind the last as the last's
+    b0 = lane == 0 ? 0 : (min(max(p.start[lane], 0), p.tokens) + up) >> log_rows;
+    n = (lane == p.n_seq - 1 ? blocks : (min(max(p.start[lane + 1], 0), p.tokens) + up) >> log_rows) - b0;
+  }
+  auto ahead = [&](int x) { return wave_total(n > x ? causal ? n - x : n : 0); };
+  if (ahead(0) != blocks) return plain;   // boundaries out of order
+  int lo = 0, hi = blocks;                // ahead(lo) > i >= ahead(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (ahead(mid) > i) lo = mid;
+    else hi = mid;
+  }
+  const int rest = i - ahead(hi);
+  const bool at = causal ? n > lo : n == hi;   // sequences that have such blocks: one each, or hi each
+  const int nth = causal ? rest : rest / hi, x = causal ? from_end ? n - 1 - lo : lo : rest % hi;
+  const uint64_t m = __ballot(at), before = ((uint64_t)1 << lane) - 1;
+  const uint64_t mine = __ballot(at && __popcll(m & before) == nth);
+  if (mine == 0) return plain;
+  return min(max(lane_value(b0 + x, __ffsll((unsigned long long)mine) - 1), 0), blocks - 1);
+}
+
 constexpr float LN2_P = 0.6931471805599453f;
 constexpr float LOG2E_P = 1.4426950408889634f;
 
@@ -66,6 +105,68 @@ __device__ __forceinline__ bf16x8 read_tr(lds_char_ptr tile, int off0, int off1,
   return __builtin_bit_cast(bf16x8, v8s{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
 }
 
+// N wave-wide copies of 1 KB from a raw buffer straight into LDS: lane i's 16 bytes at byte voff[n] of the buffer land at LDS byte
+// address dst + n step + 16 i; bytes past the buffer's end arrive as zeros.  dst and step are wave-uniform.  M0 holds the LDS address
+// and is put back (the compiler keeps it for itself).  Asynchronous, counted by vmcnt.
+template <int N>
+__device__ __forceinline__ void copy_rows(uint32_t dst, uint32_t step, lds_buffer_t buf, const uint32_t* voff) {
+  static_assert(N == 1 || N == 2 || N == 4, "copies of one statement");
+  uint32_t saved;
+#define PF_COPY_NEXT(V) "s_add_u32 m0, m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %" #V ", %3, 0 offen lds\n\t"
+#define PF_COPY_FIRST "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %3, 0 offen lds\n\t"
+  if constexpr (N == 1)
+    asm volatile(PF_COPY_FIRST "s_mov_b32 m0, %0" : "=&s"(saved) : "s"(dst), "s"(step), "s"(buf), "v"(voff[0]) : "memory", "scc");
+  else if constexpr (N == 2)
+    asm volatile(PF_COPY_FIRST PF_COPY_NEXT(5) "s_mov_b32 m0, %0" : "=&s"(saved) : "s"(dst), "s"(step), "s"(buf), "v"(voff[0]), "v"(voff[1]) : "memory", "scc");
+  else
+    asm volatile(PF_COPY_FIRST PF_COPY_NEXT(5) PF_COPY_NEXT(6) PF_COPY_NEXT(7) "s_mov_b32 m0, %0"
+                 : "=&s"(saved)
+                 : "s"(dst), "s"(step), "s"(buf), "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3])
+                 : "memory", "scc");
+#undef PF_COPY_NEXT
+#undef PF_COPY_FIRST
+}
+
+// Copies of a tile of 64 rows: of the NI = 64 d_head / 512 copies, those from `first` in steps of STEP.  One copy is 512 / d_head rows;
+// which chunk of a row a lane fetches undoes the swizzle (swz, of the row's number in the tile).  base: of the operand's head; rows
+// row0 .. row_end - 1 are read, the rest of the tile becomes zeros.  Strides are at most 2^24 elements, so a tile's offsets fit 32 bits.
+template <int DH, int STEP, class Swz>
+struct TileCopy {
+  static constexpr int CPR = DH / 8, RPI = 512 / DH, NI = 64 / RPI, N = NI / STEP;
+  static constexpr int PERIOD = STEP * RPI >= 16 ? 1 : 16 / (STEP * RPI);   // copies after which a lane's swizzle repeats
+  uint32_t off[PERIOD];
+  uint32_t ldb;
+  __device__ __forceinline__ void init(int64_t ld, int first) {
+    const int lane = threadIdx.x & 63;
+    ldb = (uint32_t)ld * 2;
+#pragma unroll
+    for (int i = 0; i < PERIOD; ++i) {
+      const int r = (first + i * STEP) * RPI + lane / CPR;
+      off[i] = (uint32_t)r * ldb + (((lane % CPR) ^ Swz::of(r)) << 4);
+    }
+  }
+  // dst: LDS address of the tile's copy `first`
+  __device__ __forceinline__ void issue(const bf16_t* base, uint32_t dst, int row0, int row_end) const {
+    const lds_buffer_t buf = lds_buffer((const char*)base + (int64_t)row0 * ldb, (uint32_t)min(row_end - row0, 64) * ldb);
+    constexpr int AT = N < 4 ? N : 4;
+#pragma unroll
+    for (int i0 = 0; i0 < N; i0 += AT) {
+      uint32_t v[AT];
+#pragma unroll
+      for (int i = 0; i < AT; ++i) v[i] = off[(i0 + i) % PERIOD] + (uint32_t)((i0 + i) / PERIOD * PERIOD * STEP * RPI) * ldb;
+      copy_rows<AT>(__builtin_amdgcn_readfirstlane(dst + (uint32_t)(i0 * STEP * 1024)), STEP * 1024, buf, v);
+    }
+  }
+};
+template <int DH>
+struct SwzRow {
+  static __device__ __forceinline__ int of(int r) { return swz_row<DH>(r); }
+};
+template <int DH>
+struct SwzCol {
+  static __device__ __forceinline__ int of(int r) { return swz_col<DH>(r); }
+};
+
 // the values of lanes l % 32 and l % 32 + 32, without LDS.  (Through an empty asm statement: a maximum of the two would
 // otherwise be folded into the first.)
 __device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
@@ -76,6 +177,9 @@ __device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
   lo = __builtin_bit_cast(float, a);
   hi = __builtin_bit_cast(float, b);
 }
+
+// Lets `kernel` have `bytes` of dynamic LDS on the current device
+hipError_t allow_lds(const void* kernel, int bytes);
 
 // bf16, d_head 64 / 128, all pointers 16-byte aligned, strides in eights
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st);

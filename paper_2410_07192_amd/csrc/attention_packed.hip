@@ -439,6 +439,8 @@ hipError_t bwd(const PackedAttn& a, const void* q, const void* k, const void* v,
 
 }  // namespace
 
+hipError_t allow_lds(const void* kernel, int bytes) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); }
+
 hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
   const bool vec = aligned16(a, {q, k, v, out});
   if (vec && by_bf16(a)) return packed_fwd_bf16(a, operands<bf16_t>(a, q, k, v), out, lse, st);

@@ -10,6 +10,8 @@
 // More heads and fewer rows read the same K/V for the same products but end nearer to the causal diagonal and to the ends of sequences.
 #include "attention_packed.h"
 
+#include <type_traits>
+
 namespace pf {
 namespace {
 
@@ -44,112 +46,49 @@ __device__ __forceinline__ void add_keys(f32x16* accO, const f32x16* p, const ch
   }
 }
 
-// One workgroup's block of rows and heads.  False, and nothing stored: a result is infinite or NaN, which hidden rows may have
-// brought in (never so with CAREFUL).  smem: two buffers of (K tile | V tile); s_span: two ints.
-struct FwdGrid {
-  int32_t heads, groups, blocks;   // of a workgroup; of the call; of rows
-  float scale_log2e;
-};
-template <int DH, int NW, bool CAREFUL>
-__device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* out, float* lse, const FwdGrid& grid, char* smem, int* s_span) {
-  constexpr int CPR = DH / 8, KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB, NI = TILE / 1024, RPI = 1024 / ROWB;
-  constexpr int PER = NI / NW;   // copies per wave of a K or V tile
-  static_assert((NW * RPI) % 16 == 0 && NI % NW == 0, "rows of one lane's copies must share their swizzle");
-
-  const int heads = grid.heads, groups = grid.groups;
-  const float scale_log2e = grid.scale_log2e;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, g = lane >> 5;
-  // head groups fastest: workgroups with the same K/V and neighbouring rows run at the same time; the last rows (causal: the
-  // long ones) first
-  const int hg = (int)(blockIdx.x % (uint32_t)groups), blk = grid.blocks - 1 - (int)(blockIdx.x / (uint32_t)groups);
-  const int hd = hg * heads + wave % heads, T = a.rows.tokens;
-  const int q_blk = (blk * (NW / heads) + wave / heads) * 32, q_row = q_blk + lr;
+// A wave's 32 rows of one head: queries, running sums and output, and the steps over a tile of 64 keys in LDS
+template <int DH>
+struct FwdRows {
+  static constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB;
   bf16x8 fq[KS];
-  {
-    const bf16_t* p = a.q + (int64_t)min(q_row, T - 1) * a.ld_q + hd * DH + g * 8;
+  f32x16 accO[DT];
+  // m_ref: reference point of the running sum and of O (scaled scores, log2 units).  In tiles that every row sees it follows the running
+  // maximum lazily: exponentials are taken against it as it stands, and it moves only when a lane's share of the tile's sum
+  // exceeds 2^7, so that most tiles compute no maximum and rescale nothing.  l_run: this lane's share of the sum, 32 of every 64 keys.
+  float m_ref, l_run, scale_log2e;
+  Span own;
+  int lr, g, v_off0, v_off1;
+
+  __device__ __forceinline__ void load(const PackedQkv<bf16_t>& a, int hd, int q_row) {
+    const bf16_t* p = a.q + (int64_t)min(q_row, a.rows.tokens - 1) * a.ld_q + hd * DH + g * 8;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) fq[kk] = as_bf16x8(*(const uint4*)(p + kk * 16));
   }
-  const Span own = keys_of(a.rows, q_blk, q_row, a.causal);
-  const int w_lo = lane_value(own.lo, 0), w_hi = lane_value(own.hi, 31);       // of the wave
-  const int in_lo = lane_value(own.lo, 31), in_hi = lane_value(own.hi, 0);     // inside them every row sees every key
-  if (tid == 0) s_span[0] = w_lo;
-  if (tid == 64 * (NW - 1)) s_span[1] = w_hi;
-  __syncthreads();
-  const int k_begin = __builtin_amdgcn_readfirstlane(s_span[0]), k_end = __builtin_amdgcn_readfirstlane(s_span[1]);
-  const int n_tiles = k_end > k_begin ? (k_end - k_begin + 63) >> 6 : 0;
-
-  const int st_row = wave * RPI + lane / CPR;
-  const bf16_t* kh = a.k + hd / a.group * DH + (((lane % CPR) ^ swz_row<DH>(st_row)) << 3);
-  const bf16_t* vh = a.v + hd / a.group * DH + (((lane % CPR) ^ swz_col<DH>(st_row)) << 3);
-  const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_ptr)smem);
-  const uint32_t ldb_k = (uint32_t)a.ld_k * 2, ldb_v = (uint32_t)a.ld_v * 2;   // bytes (strides are at most 2^30)
-  auto stage = [&](int buf, int k0) {
+  __device__ __forceinline__ void begin() {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(buf * 2 * TILE + (wave + NW * i) * 1024));
-      const uint32_t row = min(k0 + st_row + NW * i * RPI, k_end - 1);   // rows past the end repeat the last one and are hidden
-      lds_direct_load_1k(dst, (const char*)kh + (uint64_t)row * ldb_k);
-      lds_direct_load_1k(dst + TILE, (const char*)vh + (uint64_t)row * ldb_v);
-    }
-  };
-  const int v_off0 = TILE + tr_offset<DH>(lane, 0), v_off1 = TILE + tr_offset<DH>(lane, 1);   // the other two of d_head 128: 128 bytes on
-
-  f32x16 accO[DT];
-  // Reference point of the running sum and of O (scaled scores, log2 units).  It follows the running maximum lazily: it moves
-  // only when a lane's share of a tile's sum against it exceeds 2^7, so most tiles compute no maximum and rescale nothing.
-  float m_ref, l_run;   // l_run: this lane's share, 32 of every 64 keys
-  static_assert(NW * 2048 <= 2 * TILE, "the second buffer holds a careful wave's probabilities");
-  if (!CAREFUL && n_tiles > 0) stage(0, k_begin);
+    for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fq[kk]));   // waited for here, once
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fq[kk]));   // waited for here, once
+    for (int i = 0; i < DT; ++i)
 #pragma unroll
-  for (int i = 0; i < DT; ++i)
+      for (int r = 0; r < 16; ++r) accO[i][r] = 0.f;
+    m_ref = -INFINITY;
+    l_run = 0.f;
+  }
+  __device__ __forceinline__ void scores(const char* sK, f32x16* s) const {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) accO[i][r] = 0.f;
-  m_ref = -INFINITY;
-  l_run = 0.f;
-  for (int kt = 0; kt < n_tiles; ++kt) {
-    const int k0 = k_begin + kt * 64, buf = CAREFUL ? 0 : kt & 1;
-    if (CAREFUL) {
-      __syncthreads();
-      stage(0, k0);
-    }
-    // tile kt has landed (every wave waits for its own copies, then the barrier), and everyone has left the tile before it
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (!CAREFUL && kt + 1 < n_tiles) stage(buf ^ 1, k0 + 64);
-    if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
-    const char* sK = smem + buf * 2 * TILE;
-    lds_char_ptr sV = (lds_char_ptr)(lds_void_ptr)smem + buf * 2 * TILE;
-    const bool masked = k0 < in_lo || k0 + 64 > in_hi;
-    f32x16 s[2];
-    auto scores = [&] {
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int r = 0; r < 16; ++r) s[ks][r] = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[ks][r] = 0.f;
+    for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk)
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          const int r = ks * 32 + lr;
-          const uint4 fk = *(const uint4*)(sK + r * ROWB + (((kk * 2 + g) ^ swz_row<DH>(r)) << 4));
-          s[ks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fk), fq[kk], s[ks], 0, 0, 0);
-        }
-      if (masked) {
-        const int lo = own.lo - k0 - 4 * g, hi = own.hi - k0 - 4 * g;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = ks * 32 + 8 * (r >> 2) + (r & 3);
-            if (key < lo || key >= hi) s[ks][r] = -INFINITY;
-          }
+      for (int ks = 0; ks < 2; ++ks) {
+        const int r = ks * 32 + lr;
+        const uint4 fk = *(const uint4*)(sK + r * ROWB + (((kk * 2 + g) ^ swz_row<DH>(r)) << 4));
+        s[ks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fk), fq[kk], s[ks], 0, 0, 0);
       }
-    };
-    scores();
+  }
+  __device__ __forceinline__ float exponentials(f32x16* s) const {   // their sum
     const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -159,44 +98,50 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
         s[ks][r] = __builtin_amdgcn_exp2f(fmaf(s[ks][r], scale_log2e, neg_m));
         part[r & 3] += s[ks][r];
       }
-    float tot = (part[0] + part[1]) + (part[2] + part[3]);
-    // Rare: no reference point yet, or the sum against the old one is over 2^7 (also infinite or NaN): scores again, the reference
-    // point moves to the running maximum, O and the running sum are rescaled
-    if (__any(!(tot <= 128.0f) || m_ref == -INFINITY)) {
-      scores();
-      float mx0 = fmaxf(s[0][0], s[1][0]), mx1 = fmaxf(s[0][1], s[1][1]);
-#pragma unroll
-      for (int r = 2; r < 16; r += 2) {
-        mx0 = fmaxf(fmaxf(mx0, s[0][r]), s[1][r]);
-        mx1 = fmaxf(fmaxf(mx1, s[0][r + 1]), s[1][r + 1]);
+    return (part[0] + part[1]) + (part[2] + part[3]);
+  }
+  // Scores of the tile at key k0 into probabilities.  masked: not every row sees every key; fresh: nothing has been added yet.
+  __device__ __forceinline__ void probabilities(const char* sK, f32x16* s, int k0, bool masked, bool fresh) {
+    if (!(masked || fresh)) {
+      const float tot = exponentials(s);
+      if (!__any(!(tot <= 128.0f))) {   // (also infinite or NaN)
+        l_run += tot;
+        return;
       }
-      float lo, hi;
-      both_halves(fmaxf(mx0, mx1), lo, hi);
-      const float m_new = fmaxf(m_ref, fmaxf(lo, hi) * scale_log2e);
+      scores(sK, s);
+    } else if (masked) {
+      const int lo = own.lo - k0 - 4 * g, hi = own.hi - k0 - 4 * g;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = ks * 32 + 8 * (r >> 2) + (r & 3);
+          if (key < lo || key >= hi) s[ks][r] = -INFINITY;
+        }
+    }
+    float mx0 = fmaxf(s[0][0], s[1][0]), mx1 = fmaxf(s[0][1], s[1][1]);
+#pragma unroll
+    for (int r = 2; r < 16; r += 2) {
+      mx0 = fmaxf(fmaxf(mx0, s[0][r]), s[1][r]);
+      mx1 = fmaxf(fmaxf(mx1, s[0][r + 1]), s[1][r + 1]);
+    }
+    float lo, hi;
+    both_halves(fmaxf(mx0, mx1), lo, hi);
+    const float m_new = fmaxf(m_ref, fmaxf(lo, hi) * scale_log2e);
+    if (!fresh && __any(m_new > m_ref)) {
       const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);   // m_ref = -inf: 0
       l_run *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) accO[i][r] *= alpha;
-      m_ref = m_new;
-      const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
-      tot = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[ks][r] = __builtin_amdgcn_exp2f(fmaf(s[ks][r], scale_log2e, neg));
-          tot += s[ks][r];
-        }
     }
-    l_run += tot;
-    if (CAREFUL && masked) {
-      add_keys<DH>(accO, s, sK + TILE, (bf16_t*)(smem + 2 * TILE + wave * 2048), k0, own);
-      continue;
-    }
-    // O^T += V^T P^T: K step i covers keys 16 i .. 16 i + 15, operand slot (g, t) is key 16 i + 8 (t / 4) + 4 g + t % 4 =
-    // register 8 (i % 2) + t of sub-tile i / 2.  P is rounded to bf16 (half a step, 2^-8 of each), its sum is not.
+    m_ref = m_new;
+    l_run += exponentials(s);
+  }
+  // O^T += V^T P^T: K step i covers keys 16 i .. 16 i + 15, operand slot (g, t) is key 16 i + 8 (t / 4) + 4 g + t % 4 =
+  // register 8 (i % 2) + t of sub-tile i / 2.  P is rounded to bf16 (half a step, 2^-8 of each), its sum is not.
+  __device__ __forceinline__ void add(lds_char_ptr sV, const f32x16* s) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       bf16x8 fp;
@@ -209,18 +154,22 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
       }
     }
   }
-  if (!CAREFUL) {
-    bool odd = false;
+  // whether a result is infinite or NaN, which rows hidden from it may have brought in
+  __device__ __forceinline__ bool odd() const {
+    bool r_ = false;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(accO[i][r]) < INFINITY);
-    if (__syncthreads_or(odd && own.lo < own.hi)) return false;
+      for (int r = 0; r < 16; ++r) r_ = r_ || !(fabsf(accO[i][r]) < INFINITY);
+    return r_ && own.lo < own.hi;
   }
-  float lo, hi;
-  both_halves(l_run, lo, hi);
-  l_run = lo + hi;
-  if (own.lo < own.hi) {
+  __device__ __forceinline__ void sum_halves() {
+    float lo, hi;
+    both_halves(l_run, lo, hi);
+    l_run = lo + hi;
+  }
+  __device__ __forceinline__ void store(const PackedQkv<bf16_t>& a, int hd, int q_row, bf16_t* out, float* lse) const {
+    if (own.lo >= own.hi) return;
     const float inv = 1.f / l_run;   // a row whose scores are all -inf has no softmax: 0 / 0
     bf16_t* orow = out + (int64_t)q_row * a.ld_out + hd * DH;
 #pragma unroll
@@ -230,40 +179,305 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
         const float v[4] = {accO[dt][rg * 4] * inv, accO[dt][rg * 4 + 1] * inv, accO[dt][rg * 4 + 2] * inv, accO[dt][rg * 4 + 3] * inv};
         store4(orow + dt * 32 + rg * 8 + g * 4, v);
       }
-    if (lse && g == 0) lse[(int64_t)hd * T + q_row] = m_ref * LN2_P + __logf(l_run);
+    if (lse && g == 0) lse[(int64_t)hd * a.rows.tokens + q_row] = m_ref * LN2_P + __logf(l_run);
   }
+};
+
+// One workgroup's block of rows and heads.  False, and nothing stored: a result is infinite or NaN, which hidden rows may have
+// brought in (never so with CAREFUL).  smem: two buffers of (K tile | V tile); s_span: two ints.
+struct FwdGrid {
+  int32_t heads, groups, blocks, log_rows;   // of a workgroup; of the call; of rows; rows of a block
+  int32_t at_once;                             // whether all workgroups start at the same time
+  float scale_log2e;
+};
+template <int DH, int KG, bool CAREFUL>
+__device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* out, float* lse, const FwdGrid& grid, char* smem, int* s_span) {
+  constexpr int NW = 4, TILE = 64 * DH * 2, BUF = KG * 2 * TILE, DT = DH / 32, LD = DH + 4;
+  static_assert(NW * 2048 <= 2 * TILE && (KG == 1 || NW * 32 * LD * 4 <= 2 * BUF), "the second buffers hold a careful wave's probabilities, all of them O of one part");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW, part = __builtin_amdgcn_readfirstlane(tid >> 6) / NW;
+  // head groups fastest: workgroups with the same rows run at the same time
+  const int hg = (int)(blockIdx.x % (uint32_t)grid.groups);
+  const int blk = block_in_order(a.rows, (int)(blockIdx.x / (uint32_t)grid.groups), grid.blocks, grid.log_rows, a.causal, false, grid.at_once);
+  const int hd = hg * grid.heads + wave % grid.heads;
+  const int q_blk = (blk * (NW / grid.heads) + wave / grid.heads) * 32;
+  FwdRows<DH> w;
+  w.lr = lane & 31;
+  w.g = lane >> 5;
+  w.scale_log2e = grid.scale_log2e;
+  w.v_off0 = TILE + tr_offset<DH>(lane, 0);   // the other two of d_head 128: 128 bytes on
+  w.v_off1 = TILE + tr_offset<DH>(lane, 1);
+  w.load(a, hd, q_blk + w.lr);
+  w.own = keys_of(a.rows, q_blk, q_blk + w.lr, a.causal);
+  const int w_lo = lane_value(w.own.lo, 0), w_hi = lane_value(w.own.hi, 31);       // of the wave
+  const int in_lo = lane_value(w.own.lo, 31), in_hi = lane_value(w.own.hi, 0);     // inside them every row sees every key
+  if (tid == 0) s_span[0] = w_lo;
+  if (tid == 64 * (NW - 1)) s_span[1] = w_hi;   // of part 0
+  __syncthreads();
+  const int k_begin = __builtin_amdgcn_readfirstlane(s_span[0]), k_end = __builtin_amdgcn_readfirstlane(s_span[1]);
+  const int n_tiles = k_end > k_begin ? (k_end - k_begin + 63) >> 6 : 0;
+
+  const bf16_t* kh = a.k + hd / a.group * DH;
+  const bf16_t* vh = a.v + hd / a.group * DH;
+  TileCopy<DH, NW, SwzRow<DH>> copy_k;
+  TileCopy<DH, NW, SwzCol<DH>> copy_v;
+  copy_k.init(a.ld_k, wave);
+  copy_v.init(a.ld_v, wave);
+  const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_ptr)smem) + (uint32_t)(part * 2 * TILE + wave * 1024);
+  auto stage = [&](int buf, int k0) {
+    if (KG > 1 && k0 >= k_end) return;
+    copy_k.issue(kh, lds_base + (uint32_t)(buf * BUF), k0, k_end);
+    copy_v.issue(vh, lds_base + (uint32_t)(buf * BUF + TILE), k0, k_end);
+  };
+  if (!CAREFUL && n_tiles > 0) stage(0, k_begin + part * 64);
+  w.begin();
+  bool fresh = true;
+  for (int kt = part; kt - part < n_tiles; kt += KG) {   // as many steps in every part
+    const int k0 = k_begin + kt * 64, buf = CAREFUL ? 0 : (kt / KG) & 1;
+    if (CAREFUL) {
+      __syncthreads();
+      stage(0, k0);
+    }
+    // tile kt has landed (every wave waits for its own copies, then the barrier), and everyone has left the tile before it
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (!CAREFUL && k0 + KG * 64 < k_end) stage(buf ^ 1, k0 + KG * 64);
+    if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
+    const char* sK = smem + buf * BUF + part * 2 * TILE;
+    lds_char_ptr sV = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF + part * 2 * TILE;
+    const bool masked = k0 < in_lo || k0 + 64 > in_hi;
+    f32x16 s[2];
+    __builtin_amdgcn_s_setprio(1);   // the other wave of the SIMD fills the gaps
+    w.scores(sK, s);
+    __builtin_amdgcn_s_setprio(0);
+    w.probabilities(sK, s, k0, masked, fresh);
+    fresh = false;
+    if (CAREFUL && masked) {
+      add_keys<DH>(w.accO, s, sK + TILE, (bf16_t*)(smem + BUF + part * 2 * TILE + wave * 2048), k0, w.own);
+      continue;
+    }
+    __builtin_amdgcn_s_setprio(1);
+    w.add(sV, s);
+    __builtin_amdgcn_s_setprio(0);
+  }
+  if (!CAREFUL) {
+    if (__syncthreads_or(w.odd())) return false;
+  }
+  w.sum_halves();
+  if constexpr (KG == 2) {   // the second part's maximum, sum and O meet the first's
+    if (CAREFUL) __syncthreads();
+    float* sO = (float*)smem + wave * 32 * LD;
+    float* sML = (float*)(s_span + 2) + wave * 64;
+    if (part == 1) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg)
+          *(f32x4*)(sO + w.lr * LD + dt * 32 + rg * 8 + w.g * 4) =
+              f32x4{w.accO[dt][rg * 4], w.accO[dt][rg * 4 + 1], w.accO[dt][rg * 4 + 2], w.accO[dt][rg * 4 + 3]};
+      if (w.g == 0) {
+        sML[w.lr] = w.m_ref;
+        sML[32 + w.lr] = w.l_run;
+      }
+    }
+    __syncthreads();
+    if (part == 1) return true;
+    const float m1 = sML[w.lr], m = fmaxf(w.m_ref, m1);
+    const float f0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m_ref - m), f1 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m1 - m);
+    w.l_run = w.l_run * f0 + sML[32 + w.lr] * f1;
+    w.m_ref = m;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        const f32x4 x = *(const f32x4*)(sO + w.lr * LD + dt * 32 + rg * 8 + w.g * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w.accO[dt][rg * 4 + j] = w.accO[dt][rg * 4 + j] * f0 + x[j] * f1;
+      }
+  }
+  w.store(a, hd, q_blk + w.lr, out, lse);
   return true;
 }
 
 // apart from the kernel: its registers are not the kernel's concern
-template <int DH, int NW>
+template <int DH, int KG>
 __device__ __noinline__ void fwd_block_with_care(PackedQkv<bf16_t> a, bf16_t* out, float* lse, FwdGrid grid, char* smem, int* s_span) {
-  fwd_block<DH, NW, true>(a, out, lse, grid, smem, s_span);
+  fwd_block<DH, KG, true>(a, out, lse, grid, smem, s_span);
 }
 
-template <int DH, int NW>
-__global__ __launch_bounds__(64 * NW, DH == 64 ? 4 : 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out,
-                                                                                    float* __restrict__ lse, FwdGrid grid) {
-  __shared__ __align__(16) char smem[2 * 2 * 64 * DH * 2];
-  __shared__ int s_span[2];
-  if (!fwd_block<DH, NW, false>(a, out, lse, grid, smem, s_span)) fwd_block_with_care<DH, NW>(a, out, lse, grid, smem, s_span);
+template <int DH, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
+  extern __shared__ __align__(16) char dyn_smem[];   // two buffers of KG (K tile | V tile)
+  __shared__ int s_span[2 + (KG > 1 ? 256 : 0)];
+  if (!fwd_block<DH, KG, false>(a, out, lse, grid, dyn_smem, s_span)) fwd_block_with_care<DH, KG>(a, out, lse, grid, dyn_smem, s_span);
 }
 
-template <int DH, int NW>
-hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
-  int heads = 1;
-  while (heads < NW && (a.h / a.h_kv) % (heads * 2) == 0) heads *= 2;
-  const int rows = 32 * NW / heads;
-  const int64_t blocks = (a.tokens + rows - 1) / rows;
-  const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, LOG2E_P * o.scale};
-  hipLaunchKernelGGL((packed_fwd_bf16_kernel<DH, NW>), dim3((unsigned)(blocks * grid.groups)), dim3(64 * NW), 0, st, o, (bf16_t*)out, lse, grid);
+// Independent waves: each has 32 rows of one head and K/V buffers of its own, so nothing waits for another wave.  KG waves share
+// the keys of a unit (tile kt belongs to wave kt % KG) and join their (maximum, sum, O) in LDS.  For short sequences, whose
+// tiles few rows share anyway, and for few rows, where a unit's own chain over the keys is the time.
+template <int DH, int KG>
+__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_fwd_units_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out,
+                                                                                 float* __restrict__ lse, int32_t blocks, int64_t units,
+                                                                                 int32_t at_once, float scale_log2e) {
+  constexpr int DT = DH / 32, TILE = 64 * DH * 2, NI = TILE / 1024, UNITS = 4 / KG, LD = DH + 4, CPR = DH / 8;
+  constexpr int OWN = 2 * TILE + 2048;   // K tile | V tile | probabilities of a careful wave; later O
+  static_assert(32 * LD * 4 <= OWN, "O of a wave fits its buffers");
+  extern __shared__ __align__(16) char dyn_smem[];
+  __shared__ float sM[4][32], sL[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % KG;
+  const int64_t unit = (int64_t)blockIdx.x * UNITS + wave / KG;
+  const bool real = unit < units;                    // heads fastest
+  const int hd = real ? (int)(unit % a.h) : 0;
+  const int q_blk = real ? block_in_order(a.rows, (int)(unit / a.h), blocks, 5, a.causal, false, at_once) * 32 : 0;
+  FwdRows<DH> w;
+  w.lr = lane & 31;
+  w.g = lane >> 5;
+  w.scale_log2e = scale_log2e;
+  w.v_off0 = TILE + tr_offset<DH>(lane, 0);
+  w.v_off1 = TILE + tr_offset<DH>(lane, 1);
+  w.load(a, hd, q_blk + w.lr);
+  w.own = keys_of(a.rows, q_blk, q_blk + w.lr, a.causal);
+  if (!real) w.own.hi = w.own.lo;
+  const int k_begin = lane_value(w.own.lo, 0), k_end = lane_value(w.own.hi, 31);
+  const int in_lo = lane_value(w.own.lo, 31), in_hi = lane_value(w.own.hi, 0);
+  const int n_tiles = real && k_end > k_begin ? (k_end - k_begin + 63) >> 6 : 0;
+
+  char* const mine = dyn_smem + wave * OWN;
+  lds_char_ptr sV = (lds_char_ptr)(lds_void_ptr)dyn_smem + wave * OWN;
+  const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_ptr)dyn_smem) + (uint32_t)(wave * OWN);
+  const bf16_t* kh = a.k + hd / a.group * DH;
+  const bf16_t* vh = a.v + hd / a.group * DH;
+  TileCopy<DH, 1, SwzRow<DH>> copy_k;
+  TileCopy<DH, 1, SwzCol<DH>> copy_v;
+  copy_k.init(a.ld_k, 0);
+  copy_v.init(a.ld_v, 0);
+  auto walk = [&](auto careful_) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+    if (part < n_tiles) {
+      copy_k.issue(kh, lds_base, k_begin + part * 64, k_end);
+      copy_v.issue(vh, lds_base + TILE, k_begin + part * 64, k_end);
+    }
+    w.begin();
+#pragma unroll 1
+    for (int kt = part; kt < n_tiles; kt += KG) {
+      const int k0 = k_begin + kt * 64;
+      const bool more = kt + KG < n_tiles, masked = k0 < in_lo || k0 + 64 > in_hi;
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NI) : "memory");   // K of the tile has landed; V's NI copies may be on their way
+      f32x16 s[2];
+      w.scores(mine, s);
+      w.probabilities(mine, s, k0, masked, kt == part);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K has been read: the next tile's may come
+      if (more) {
+        copy_k.issue(kh, lds_base, k0 + KG * 64, k_end);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NI) : "memory");   // V has landed
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      if (CAREFUL && masked) add_keys<DH>(w.accO, s, mine + TILE, (bf16_t*)(mine + 2 * TILE), k0, w.own);
+      else w.add(sV, s);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy_v.issue(vh, lds_base + TILE, k0 + KG * 64, k_end);
+    }
+  };
+  walk(std::false_type{});
+  if (__any(w.odd())) walk(std::true_type{});
+  w.sum_halves();
+  if constexpr (KG == 1) {
+    w.store(a, hd, q_blk + w.lr, out, lse);
+  } else {
+    if (w.g == 0) {
+      sM[wave][w.lr] = w.m_ref;
+      sL[wave][w.lr] = w.l_run;
+    }
+    float* sO = (float*)mine;   // this wave's reads of its buffers are complete
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg)
+        *(f32x4*)(sO + w.lr * LD + dt * 32 + rg * 8 + w.g * 4) =
+            f32x4{w.accO[dt][rg * 4], w.accO[dt][rg * 4 + 1], w.accO[dt][rg * 4 + 2], w.accO[dt][rg * 4 + 3]};
+    const uint64_t live = __ballot(w.own.lo < w.own.hi);
+    __syncthreads();
+    const int first = wave / KG * KG;   // the unit's waves share its rows
+    for (int e = part * 64 + lane; e < 32 * CPR; e += 64 * KG) {
+      const int q = e / CPR, c = e % CPR * 8;
+      if (!((live >> q) & 1)) continue;
+      float mq = sM[first][q];
+#pragma unroll
+      for (int i = 1; i < KG; ++i) mq = fmaxf(mq, sM[first + i][q]);
+      float lq = 0.f, o[8] = {};
+#pragma unroll
+      for (int i = 0; i < KG; ++i) {
+        const float f = mq == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sM[first + i][q] - mq);   // 0 for a wave that met no key
+        const float* po = (const float*)(dyn_smem + (first + i) * OWN) + q * LD + c;
+        const f32x4 x = *(const f32x4*)po, y = *(const f32x4*)(po + 4);
+        lq += f * sL[first + i][q];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[j] += f * x[j];
+          o[4 + j] += f * y[j];
+        }
+      }
+      const float inv = 1.f / lq;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] *= inv;
+      store8(out + (int64_t)(q_blk + q) * a.ld_out + hd * DH + c, o);
+      if (lse && c == 0) lse[(int64_t)hd * a.rows.tokens + q_blk + q] = mq * LN2_P + __logf(lq);
+    }
+  }
+}
+
+template <int DH, int KG>
+hipError_t launch_units(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+  constexpr int lds = 4 * (2 * 64 * DH * 2 + 2048);
+  hipError_t e = allow_lds((const void*)packed_fwd_units_kernel<DH, KG>, lds);
+  if (e != hipSuccess) return e;
+  const int64_t blocks = (a.tokens + 31) / 32, units = blocks * a.h;
+  hipLaunchKernelGGL((packed_fwd_units_kernel<DH, KG>), dim3((unsigned)((units * KG + 3) / 4)), dim3(256), lds, st, o, (bf16_t*)out, lse, (int32_t)blocks, units, units * KG / 4 <= (DH == 64 ? 512 : 256),
+                     LOG2E_P * o.scale);
   return hipGetLastError();
+}
+
+template <int DH, int KG>
+hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+  constexpr int lds = 2 * KG * 2 * 64 * DH * 2;
+  hipError_t e = allow_lds((const void*)packed_fwd_bf16_kernel<DH, KG>, lds);
+  if (e != hipSuccess) return e;
+  int heads = 1;
+  while (heads < 4 && (a.h / a.h_kv) % (heads * 2) == 0) heads *= 2;
+  const int rows = 128 / heads, log_rows = __builtin_ctz(rows);
+  const int64_t blocks = (a.tokens + rows - 1) / rows;
+  const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, log_rows, blocks * (a.h / heads) * KG <= 512, LOG2E_P * o.scale};
+  hipLaunchKernelGGL((packed_fwd_bf16_kernel<DH, KG>), dim3((unsigned)(blocks * grid.groups)), dim3(256 * KG), lds, st, o, (bf16_t*)out, lse, grid);
+  return hipGetLastError();
+}
+
+// 1, 2, 4: independent waves with that many to a unit's keys; 0: shared tiles
+int fwd_form(const PackedAttn& a) {
+  const int64_t units = (a.tokens + 31) / 32 * a.h;
+  if (units <= (a.dh == 64 ? 1024 : 384)) return 4;
+  if (a.dh == 64 && units <= 4096) return 1;
+  return 0;
 }
 
 }  // namespace
 
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
-  return a.dh == 64 ? launch<64, 8>(a, o, out, lse, st) : launch<128, 4>(a, o, out, lse, st);
+  int form = fwd_form(a);
+  if (a.dh == 64) {
+    switch (form) {
+      case 1: return launch_units<64, 1>(a, o, out, lse, st);
+      case 2: return launch_units<64, 2>(a, o, out, lse, st);
+      case 4: return launch_units<64, 4>(a, o, out, lse, st);
+      default: return launch<64, 1>(a, o, out, lse, st);
+    }
+  }
+  switch (form) {
+    case 1: return launch_units<128, 1>(a, o, out, lse, st);
+    case 2: return launch_units<128, 2>(a, o, out, lse, st);
+    case 4: return launch_units<128, 4>(a, o, out, lse, st);
+    case 8: return launch<128, 2>(a, o, out, lse, st);
+    default: return launch<128, 1>(a, o, out, lse, st);
+  }
 }
 
 }  // namespace pf

@@ -10,7 +10,7 @@ bool bad_dtype(int32_t dt) { return dt != PF_DTYPE_F32 && dt != PF_DTYPE_BF16; }
 
 // Rows that fit 32-bit row numbers with a block of room behind them
 constexpr int64_t MAX_ROWS = 0x7fffffff - 512;
-constexpr int64_t MAX_STRIDE = 1 << 30;   // its bytes fit 32 bits
+constexpr int64_t MAX_STRIDE = 1 << 24;   // the bytes of 64 rows fit 32 bits
 // A launch has at most 2^32 threads: 256 for every 32 rows of a head
 constexpr int64_t MAX_BLOCKS = 1 << 22;
 
@@ -33,7 +33,7 @@ int32_t attention_args(const char* who, const pf_packed_attn* d, const int32_t* 
   a->ld_v = d->ld_v ? d->ld_v : wk;
   a->ld_out = d->ld_out ? d->ld_out : wq;
   if (a->ld_q < wq || a->ld_k < wk || a->ld_v < wk || a->ld_out < wq || std::max(std::max(a->ld_q, a->ld_k), std::max(a->ld_v, a->ld_out)) > MAX_STRIDE)
-    return pf::fail(PF_ERR_ARG, "%s: bad argument (rows overlap, or a stride over 2^30)", who);
+    return pf::fail(PF_ERR_ARG, "%s: bad argument (rows overlap, or a stride over 2^24)", who);
   if ((d->tokens + 31) / 32 * d->n_heads > MAX_BLOCKS)
     return pf::fail(PF_ERR_ARG, "%s: bad argument (tokens * n_heads is more than 2^27)", who);
   a->tokens = d->tokens;

@@ -41,25 +41,39 @@ __device__ __forceinline__ int packed_count(const int32_t* start, int n, int row
 // The rows of the sequence that `row` is in; r0: the first row that a lane of the wave asks for, the same in all of them, and
 // r0 <= row < r0 + 64.  A row of no sequence gets an empty span: at the first boundary before it, at the last behind it (both
 // ends of the spans of ascending rows ascend).  0 <= lo <= hi <= tokens whatever `start` holds.
+// The boundary before r0 and the 63 that follow it are one load; those up to r0 + 63 are then gone through one by one.
 __device__ __forceinline__ Span packed_span(const PackedRows& p, int r0, int row) {
   if (p.start == nullptr) return row < p.tokens ? Span{0, p.tokens} : Span{p.tokens, p.tokens};
-  const int n = p.n_seq + 1;
-  int c = packed_count(p.start, n, r0);
-  if (c < n && p.start[c] <= r0 + 63) {   // a boundary among the rows asked for: each lane looks for its own
-    int lo = c, hi = n;
-    if (c + 64 < n && p.start[c + 64] > r0 + 63) hi = c + 64;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (p.start[mid] <= row) lo = mid + 1;
-      else hi = mid;
-    }
-    c = lo;
+  const int lane = threadIdx.x & 63, n = p.n_seq + 1;
+  int base = 0;   // of the boundaries in the lanes
+  int w = p.start[min(lane, n - 1)];
+  if (n > 64) {
+    base = max(packed_count(p.start, n, r0) - 1, 0);
+    w = p.start[min(base + lane, n - 1)];
   }
-  if (c == 0 || c == n || row >= p.tokens) {
-    const int x = min(max(p.start[c == 0 ? 0 : p.n_seq], 0), p.tokens);
+  int at = __popcll(__ballot(base + lane < n && w <= r0));   // boundaries of the lanes that are <= r0: the span begins at the last
+  int lo = at > 0 ? __builtin_amdgcn_readlane(w, at - 1) : INT32_MIN;   // INT32_MIN: before the first sequence
+  int hi, begin = lo, end;
+  for (bool first = true;; first = false) {   // [lo, hi): rows between two boundaries
+    if (at == 64) {
+      base += 64;
+      at = 0;
+      w = p.start[min(base + lane, n - 1)];
+    }
+    hi = base + at < n ? __builtin_amdgcn_readlane(w, at) : INT32_MAX;   // INT32_MAX: behind the last
+    if (first || row >= lo) {
+      begin = lo;
+      end = hi;
+    }
+    if (hi > r0 + 63 || base + at >= n) break;
+    lo = hi;
+    ++at;
+  }
+  if (begin == INT32_MIN || end == INT32_MAX || row >= p.tokens) {
+    const int x = min(max(begin == INT32_MIN ? end : begin, 0), p.tokens);
     return Span{x, x};
   }
-  return Span{min(max(p.start[c - 1], 0), row), min(max(p.start[c], row + 1), p.tokens)};
+  return Span{min(max(begin, 0), row), min(max(end, row + 1), p.tokens)};
 }
 
 }  // namespace pf
