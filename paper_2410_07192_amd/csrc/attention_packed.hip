@@ -449,7 +449,8 @@ hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* 
 #undef PF_FWD
 }
 
-int64_t attention_packed_bwd_bytes(const PackedAttn& a) { return (int64_t)a.h * a.tokens * 4; }
+static int64_t dsum_bytes(const PackedAttn& a) { return ((int64_t)a.h * a.tokens * 4 + 255) / 256 * 256; }
+int64_t attention_packed_bwd_bytes(const PackedAttn& a) { return dsum_bytes(a) + (by_bf16(a) ? packed_bwd_bf16_bytes(a) : 0); }
 
 hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* out, const void* dout,
                                 const float* lse, void* dq, void* dk, void* dv, void* workspace, hipStream_t st) {
@@ -470,6 +471,8 @@ hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* 
 #undef PF_PREP
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (vec && by_bf16(a))
+    return packed_bwd_bf16(a, operands<bf16_t>(a, q, k, v), dout, lse, dsum, dq, dk, dv, (float*)((char*)workspace + dsum_bytes(a)), st);
 #define PF_BWD(T, D, V) bwd<T, D, V>(a, q, k, v, dout, lse, dsum, dq, dk, dv, st)
   PF_BY_SHAPE(PF_BWD);
 #undef PF_BWD

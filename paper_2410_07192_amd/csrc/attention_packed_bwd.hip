@@ -1,0 +1,434 @@
+// Attention backward on packed sequences, bf16, d_head 64 or 128, on the 32x32x16 bf16 MFMA (gfx950).
+//
+//   P = exp(scale S - lse), dP = dO V^T, dS = P (dP - D), D = rowsum(dO O)
+//   dV = P^T dO, dK = scale dS^T Q (both summed over the query heads of a group), dQ = scale dS K
+//
+// Two launches that each own their results (no atomics):
+//  * dK/dV: a workgroup has 128 keys of a K/V head, a wave 32 of them with K and V as "B" operands in registers, and walks the
+//    tiles of 64 queries of the group's heads.  S = Q K^T and dP = dO V^T put one key and 32 of a tile's 64 queries into a lane:
+//    the "B" operands of dV^T += dO^T P and dK^T += Q^T dS, whose "A" operands come out of the same row-major tiles by the
+//    transposing LDS load.  Where keys and K/V heads are too few for the card, the heads of a group are dealt out to several
+//    workgroups, whose fp32 sums a third launch adds up.
+//  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
+// Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h and the forward kernel; here
+// too a result with an infinity or NaN is computed a second time with care.
+#include "attention_packed.h"
+
+#include <type_traits>
+
+namespace pf {
+namespace {
+
+// Swizzle of tiles that are read both ways: for one chunk per lane from consecutive rows a bijection of the bank phases, and the
+// 32-byte pairs of four consecutive rows apart for the transposing read.  Depends on row % 16 only.
+template <int DH>
+struct SwzBoth {
+  static __device__ __forceinline__ int of(int r) {
+    if (DH == 64) {
+      const int x = (r >> 1) & 7;
+      return ((x & 1) << 1) | ((x >> 1) & 1) | (x & 4);
+    }
+    const int x = r & 15;
+    return (x & 8) | ((x & 3) << 1) | ((x >> 2) & 1);
+  }
+};
+// byte offsets of a lane's two transposing reads, columns from 32 dt, K step 0 (tr_offset, with this swizzle: rows 8 apart differ)
+template <int DH>
+__device__ __forceinline__ void tr_offsets(int lane, int off[][2]) {
+  const int p = lane & 15, g = lane >> 5;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int row = 8 * r + 4 * g + (p >> 2), c = dt * 4 + ((lane >> 4) & 1) * 2 + ((p & 3) >> 1);
+      off[dt][r] = row * DH * 2 + ((c ^ SwzBoth<DH>::of(row)) << 4) + 8 * (p & 1) - (r ? 8 * DH * 2 : 0);   // read_tr adds the 8 rows
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ bool not_finite(const f32x16* acc) {
+  bool r_ = false;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) r_ = r_ || !(fabsf(acc[i][r]) < INFINITY);
+  return r_;
+}
+
+struct BwdArgs {
+  PackedQkv<bf16_t> o;
+  const bf16_t* dout;
+  const float *lse, *dsum;
+  bf16_t *dq, *dk, *dv;
+  float* partial;                              // [split][dK, dV][tokens][K/V heads * d_head], or null with one split
+  int32_t blocks, splits, heads, at_once;      // blocks of rows; parts of a group's heads (dK/dV); heads of a workgroup (dQ)
+  float scale_log2e;
+};
+
+// ---- dK, dV ------------------------------------------------------------------------------------------------------------------
+template <int DH>
+__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_kernel(BwdArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB;
+  constexpr int BUF = 2 * TILE + 512;   // Q tile | dO tile | lse (log2 units) of the 64 queries | D
+  extern __shared__ __align__(16) char smem[];   // two buffers
+  __shared__ int s_span[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
+  const int n_kv = a.o.h / a.o.group, T = a.o.rows.tokens;
+  // K/V heads and splits fastest: workgroups with the same rows run at the same time
+  const uint32_t per = (uint32_t)(n_kv * a.splits);
+  const int hk = (int)(blockIdx.x % per) % n_kv, split = (int)(blockIdx.x % per) / n_kv;
+  const int k_blk = block_in_order(a.o.rows, (int)(blockIdx.x / per), a.blocks, 7, a.o.causal, true, a.at_once) * 128;
+  const int key = k_blk + wave * 32 + lr;
+  bf16x8 fk[KS], fv[KS];
+  {
+    const int row = min(key, T - 1);
+    const bf16_t* pk = a.o.k + (int64_t)row * a.o.ld_k + hk * DH + g * 8;
+    const bf16_t* pv = a.o.v + (int64_t)row * a.o.ld_v + hk * DH + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      fk[kk] = as_bf16x8(*(const uint4*)(pk + kk * 16));
+      fv[kk] = as_bf16x8(*(const uint4*)(pv + kk * 16));
+    }
+  }
+  const Span own = queries_of(a.o.rows, k_blk + wave * 32, key, a.o.causal);
+  const int w_lo = lane_value(own.lo, 0), w_hi = lane_value(own.hi, 31);
+  const int in_lo = lane_value(own.lo, 31), in_hi = lane_value(own.hi, 0);
+  if (tid == 0) s_span[0] = w_lo;
+  if (tid == 192) s_span[1] = w_hi;
+  __syncthreads();
+  const int q_begin = __builtin_amdgcn_readfirstlane(s_span[0]), q_end = __builtin_amdgcn_readfirstlane(s_span[1]);
+  const int tiles = q_end > q_begin ? (q_end - q_begin + 63) >> 6 : 0;
+  const int h0 = hk * a.o.group + a.o.group * split / a.splits, h1 = hk * a.o.group + a.o.group * (split + 1) / a.splits;
+
+  TileCopy<DH, 4, SwzBoth<DH>> copy_q, copy_d;
+  copy_q.init(a.o.ld_q, wave);
+  copy_d.init(a.o.ld_out, wave);
+  const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_ptr)smem) + (uint32_t)(wave * 1024);
+  auto stage = [&](int buf, int hd, int q0) {
+    copy_q.issue(a.o.q + hd * DH, lds_base + (uint32_t)(buf * BUF), q0, q_end);
+    copy_d.issue(a.dout + hd * DH, lds_base + (uint32_t)(buf * BUF + TILE), q0, q_end);
+  };
+  // threads 0..63 carry lse, 64..127 carry D of the tile's queries (the others repeat them and write nothing)
+  auto load_ld = [&](int hd, int q0) { return ((tid & 64) ? a.dsum : a.lse)[(int64_t)hd * T + min(q0 + (tid & 63), q_end - 1)]; };
+  auto write_ld = [&](int buf, float v) {
+    if (tid < 128) *(float*)(smem + buf * BUF + 2 * TILE + tid * 4) = tid < 64 ? v * LOG2E_P : v;
+  };
+  int t_off[DT][2];
+  tr_offsets<DH>(lane, t_off);
+  f32x16 accK[DT], accV[DT];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fk[kk]), "v"(fv[kk]));   // waited for here, once
+  const int steps = tiles * (h1 - h0);
+  auto walk = [&](auto careful_) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
+    float ld = 0.f;
+    int hd = h0, q0 = q_begin;
+    if (steps > 0) {
+      stage(0, hd, q0);
+      ld = load_ld(hd, q0);
+    }
+    for (int it = 0; it < steps; ++it) {
+      const int buf = it & 1, q_now = q0;
+      write_ld(buf, ld);   // the buffer was last read before the barrier of the previous step
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      q0 += 64;
+      if (q0 >= q_end) {
+        q0 = q_begin;
+        ++hd;
+      }
+      if (it + 1 < steps) {
+        stage(buf ^ 1, hd, q0);
+        ld = load_ld(hd, q0);
+      }
+      if (q_now + 64 <= w_lo || q_now >= w_hi) continue;   // none of the wave's keys is seen from the tile
+      const char* sQ = smem + buf * BUF;
+      const char* sdO = sQ + TILE;
+      const float* sL = (const float*)(sQ + 2 * TILE);
+      lds_char_ptr tQ = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
+      lds_char_ptr tdO = tQ + TILE;
+      const bool masked = q_now < in_lo || q_now + 64 > in_hi;
+      const int lo = own.lo - q_now, hi = own.hi - q_now;
+      f32x16 P[2], dS[2];
+#pragma unroll
+      for (int qs = 0; qs < 2; ++qs) {
+        f32x16 aS, aP;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const int r = qs * 32 + lr;
+          const int o = r * ROWB + (((kk * 2 + g) ^ SwzBoth<DH>::of(r)) << 4);
+          aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sQ + o)), fk[kk], aS, 0, 0, 0);
+          aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
+        }
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg) {
+          const int qi = qs * 32 + 8 * rg + 4 * g;
+          const f32x4 L4 = *(const f32x4*)(sL + qi), D4 = *(const f32x4*)(sL + 64 + qi);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(aS[rg * 4 + j], a.scale_log2e, -L4[j]));
+            P[qs][rg * 4 + j] = p;
+            dS[qs][rg * 4 + j] = p * (aP[rg * 4 + j] - D4[j]);
+          }
+        }
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int q = qs * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+            if (q < lo || q >= hi) P[qs][r] = dS[qs][r] = 0.f;
+          }
+        }
+      }
+      if (CAREFUL && masked) {
+        auto off = [&](int dt, int r) { return t_off[dt][r]; };
+        add_with_care<DH>(accV, P, tdO, off, lo, hi);
+        add_with_care<DH>(accK, dS, tQ, off, lo, hi);
+        continue;
+      }
+      // contraction over the 64 queries: K step i covers queries 16 i .. 16 i + 15, operand slot (g, t) is query
+      // 16 i + 8 (t / 4) + 4 g + t % 4 = register 8 (i % 2) + t of sub-tile i / 2
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf16x8 fp, fds;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          fp[t] = (__bf16)P[i >> 1][8 * (i & 1) + t];
+          fds[t] = (__bf16)dS[i >> 1][8 * (i & 1) + t];
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp, accV[dt], 0, 0, 0);
+          accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds, accK[dt], 0, 0, 0);
+        }
+      }
+    }
+  };
+  walk(std::false_type{});
+  if (__syncthreads_or((not_finite<DT>(accK) || not_finite<DT>(accV)) && own.lo < own.hi)) walk(std::true_type{});
+  if (own.lo >= own.hi) return;
+  if (a.partial == nullptr) {
+    bf16_t* pk = a.dk + (int64_t)key * a.o.ld_k + hk * DH;
+    bf16_t* pv = a.dv + (int64_t)key * a.o.ld_v + hk * DH;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        float vk[4], vv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          vk[j] = accK[dt][rg * 4 + j] * a.o.scale;
+          vv[j] = accV[dt][rg * 4 + j];
+        }
+        store4(pk + dt * 32 + rg * 8 + g * 4, vk);
+        store4(pv + dt * 32 + rg * 8 + g * 4, vv);
+      }
+  } else {
+    float* pk = a.partial + ((int64_t)split * 2 * T + key) * (n_kv * DH) + hk * DH;
+    float* pv = pk + (int64_t)T * (n_kv * DH);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        *(f32x4*)(pk + dt * 32 + rg * 8 + g * 4) = f32x4{accK[dt][rg * 4], accK[dt][rg * 4 + 1], accK[dt][rg * 4 + 2], accK[dt][rg * 4 + 3]};
+        *(f32x4*)(pv + dt * 32 + rg * 8 + g * 4) = f32x4{accV[dt][rg * 4], accV[dt][rg * 4 + 1], accV[dt][rg * 4 + 2], accV[dt][rg * 4 + 3]};
+      }
+  }
+}
+
+// dK, dV from the splits' sums: eight columns a thread, rows that are in a sequence
+template <int DH>
+__global__ __launch_bounds__(256) void packed_bwd_join_kernel(BwdArgs a) {
+  const int n_kv = a.o.h / a.o.group, T = a.o.rows.tokens, per = n_kv * DH / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int row = (int)(i / per), c = (int)(i % per) * 8;
+  const int first = a.o.rows.start ? a.o.rows.start[0] : 0, last = a.o.rows.start ? a.o.rows.start[a.o.rows.n_seq] : T;
+  if (i >= (int64_t)T * per || row < first || row >= last) return;
+  const bool is_v = blockIdx.y != 0;
+  const float* p = a.partial + ((int64_t)(is_v ? T : 0) + row) * (n_kv * DH) + c;
+  float x[8];
+  load8(p, x);
+  for (int s = 1; s < a.splits; ++s) {
+    float y[8];
+    load8(p + (int64_t)s * 2 * T * (n_kv * DH), y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] += y[j];
+  }
+  if (!is_v) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= a.o.scale;
+    store8(a.dk + (int64_t)row * a.o.ld_k + c, x);
+  } else {
+    store8(a.dv + (int64_t)row * a.o.ld_v + c, x);
+  }
+}
+
+// ---- dQ ----------------------------------------------------------------------------------------------------------------------
+template <int DH>
+__global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
+  extern __shared__ __align__(16) char smem[];   // two buffers
+  __shared__ int s_span[2];
+  constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB, BUF = 2 * TILE;   // K tile | V tile
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
+  const int T = a.o.rows.tokens, groups = a.o.h / a.heads, tiles_of_rows = 4 / a.heads;
+  const int hg = (int)(blockIdx.x % (uint32_t)groups);
+  const int blk = block_in_order(a.o.rows, (int)(blockIdx.x / (uint32_t)groups), a.blocks, 5 + (tiles_of_rows >> 1), a.o.causal, false, a.at_once);
+  const int hd = hg * a.heads + wave % a.heads, q_blk = (blk * tiles_of_rows + wave / a.heads) * 32;
+  const int q_row = q_blk + lr, q_cl = min(q_row, T - 1);
+  bf16x8 fq[KS], fd[KS];
+  {
+    const bf16_t* pq = a.o.q + (int64_t)q_cl * a.o.ld_q + hd * DH + g * 8;
+    const bf16_t* pd = a.dout + (int64_t)q_cl * a.o.ld_out + hd * DH + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      fq[kk] = as_bf16x8(*(const uint4*)(pq + kk * 16));
+      fd[kk] = as_bf16x8(*(const uint4*)(pd + kk * 16));
+    }
+  }
+  const float neg_l = -a.lse[(int64_t)hd * T + q_cl] * LOG2E_P, D = a.dsum[(int64_t)hd * T + q_cl];
+  const Span own = keys_of(a.o.rows, q_blk, q_row, a.o.causal);
+  const int w_lo = lane_value(own.lo, 0), w_hi = lane_value(own.hi, 31);
+  const int in_lo = lane_value(own.lo, 31), in_hi = lane_value(own.hi, 0);
+  if (tid == 0) s_span[0] = w_lo;
+  if (tid == 192) s_span[1] = w_hi;
+  __syncthreads();
+  const int k_begin = __builtin_amdgcn_readfirstlane(s_span[0]), k_end = __builtin_amdgcn_readfirstlane(s_span[1]);
+  const int n_tiles = k_end > k_begin ? (k_end - k_begin + 63) >> 6 : 0;
+
+  const bf16_t* kh = a.o.k + hd / a.o.group * DH;
+  const bf16_t* vh = a.o.v + hd / a.o.group * DH;
+  TileCopy<DH, 4, SwzBoth<DH>> copy_k;
+  TileCopy<DH, 4, SwzRow<DH>> copy_v;
+  copy_k.init(a.o.ld_k, wave);
+  copy_v.init(a.o.ld_v, wave);
+  const uint32_t lds_base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_ptr)smem) + (uint32_t)(wave * 1024);
+  auto stage = [&](int buf, int k0) {
+    copy_k.issue(kh, lds_base + (uint32_t)(buf * BUF), k0, k_end);
+    copy_v.issue(vh, lds_base + (uint32_t)(buf * BUF + TILE), k0, k_end);
+  };
+  int t_off[DT][2];
+  tr_offsets<DH>(lane, t_off);
+  f32x16 acc[DT];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fq[kk]), "v"(fd[kk]));   // waited for here, once
+  asm volatile("" ::"v"(neg_l), "v"(D));
+  auto walk = [&](auto careful_) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+    if (n_tiles > 0) stage(0, k_begin);
+    for (int kt = 0; kt < n_tiles; ++kt) {
+      const int k0 = k_begin + kt * 64, buf = kt & 1;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (kt + 1 < n_tiles) stage(buf ^ 1, k0 + 64);
+      if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
+      const char* sK = smem + buf * BUF;
+      const char* sV = sK + TILE;
+      lds_char_ptr tK = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
+      const bool masked = k0 < in_lo || k0 + 64 > in_hi;
+      const int lo = own.lo - k0, hi = own.hi - k0;
+      f32x16 dS[2];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        f32x16 aS, aP;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const int r = ks * 32 + lr, c = kk * 2 + g;
+          aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sK + r * ROWB + ((c ^ SwzBoth<DH>::of(r)) << 4))), fq[kk], aS, 0, 0, 0);
+          aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sV + r * ROWB + ((c ^ swz_row<DH>(r)) << 4))), fd[kk], aP, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dS[ks][r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = ks * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+            if (key < lo || key >= hi) dS[ks][r] = 0.f;
+          }
+        }
+      }
+      if (CAREFUL && masked) {
+        add_with_care<DH>(acc, dS, tK, [&](int dt, int r) { return t_off[dt][r]; }, lo, hi);
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf16x8 fds;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) fds[t] = (__bf16)dS[i >> 1][8 * (i & 1) + t];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tK, t_off[dt][0], t_off[dt][1], i), fds, acc[dt], 0, 0, 0);
+      }
+    }
+  };
+  walk(std::false_type{});
+  if (__syncthreads_or(not_finite<DT>(acc) && own.lo < own.hi)) walk(std::true_type{});
+  if (own.lo >= own.hi) return;
+  bf16_t* row = a.dq + (int64_t)q_row * a.o.ld_q + hd * DH;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg) {
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = acc[dt][rg * 4 + j] * a.o.scale;
+      store4(row + dt * 32 + rg * 8 + g * 4, v);
+    }
+}
+
+// parts of a group's heads in dK/dV: as many as give every CU two workgroups
+int splits_of(const PackedAttn& a) {
+  const int group = a.h / a.h_kv;
+  const int64_t units = (a.tokens + 127) / 128 * a.h_kv;
+  int s = 1;
+  while (s < group && units * s < 512) ++s;
+  return s;
+}
+
+template <int DH>
+hipError_t run(const PackedAttn& a, BwdArgs b, hipStream_t st) {
+  constexpr int lds_dkv = 2 * (2 * 64 * DH * 2 + 512), lds_dq = 2 * 2 * 64 * DH * 2;
+  hipError_t e = allow_lds((const void*)packed_bwd_dkv_bf16_kernel<DH>, lds_dkv);
+  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_dq_bf16_kernel<DH>, lds_dq);
+  if (e != hipSuccess) return e;
+  b.blocks = (int32_t)((a.tokens + 127) / 128);
+  int64_t grid = (int64_t)b.blocks * a.h_kv * b.splits;
+  b.at_once = grid <= (DH == 64 ? 512 : 256);
+  hipLaunchKernelGGL(packed_bwd_dkv_bf16_kernel<DH>, dim3((unsigned)grid), dim3(256), lds_dkv, st, b);
+  if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
+  b.heads = 1;
+  while (b.heads < 4 && (a.h / a.h_kv) % (b.heads * 2) == 0) b.heads *= 2;
+  const int rows = 128 / b.heads;
+  b.blocks = (int32_t)((a.tokens + rows - 1) / rows);
+  grid = (int64_t)b.blocks * (a.h / b.heads);
+  b.at_once = grid <= 512;
+  hipLaunchKernelGGL(packed_bwd_dq_bf16_kernel<DH>, dim3((unsigned)grid), dim3(256), lds_dq, st, b);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t packed_bwd_bf16_bytes(const PackedAttn& a) {
+  const int s = splits_of(a);
+  return s > 1 ? (int64_t)s * 2 * a.tokens * a.h_kv * a.dh * 4 : 0;
+}
+
+hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
+                           void* dv, float* partial, hipStream_t st) {
+  BwdArgs b{o, (const bf16_t*)dout, lse, dsum, (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, nullptr, 0, splits_of(a), 0, 0, LOG2E_P * o.scale};
+  if (b.splits > 1) b.partial = partial;
+  return a.dh == 64 ? run<64>(a, b, st) : run<128>(a, b, st);
+}
+
+}  // namespace pf

@@ -15,37 +15,6 @@
 namespace pf {
 namespace {
 
-// O += P V for a tile that not every row sees as a whole, key by key and visible ones only: 0 (hidden) times an infinity or NaN
-// of another row's V would be NaN.  p: the probabilities as the products left them; sp: 2 KiB of LDS of this wave.
-template <int DH>
-__device__ __forceinline__ void add_keys(f32x16* accO, const f32x16* p, const char* sV, bf16_t* sp, int k0, Span own) {
-  constexpr int DT = DH / 32, ROWB = DH * 2;
-  const int lane = threadIdx.x & 63, lr = lane & 31, g = lane >> 5;
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // within the wave: its LDS instructions execute in order
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sp[(8 * (r >> 2) + 4 * g + (r & 3)) * 32 + lr] = from_f32<bf16_t>(p[ks][r]);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 1
-    for (int i = 0; i < 32; ++i) {
-      const int key = ks * 32 + i;
-      if (k0 + key < own.lo || k0 + key >= own.hi) continue;
-      const float w = to_f32(sp[i * 32 + lr]);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-          asm volatile("" ::: "memory");   // a few registers are enough here
-          float x[4];
-          load4((const bf16_t*)(sV + key * ROWB + (((dt * 4 + rg) ^ swz_col<DH>(i)) << 4) + 8 * g), x);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) accO[dt][rg * 4 + j] = fmaf(w, x[j], accO[dt][rg * 4 + j]);
-        }
-    }
-  }
-}
-
 // A wave's 32 rows of one head: queries, running sums and output, and the steps over a tile of 64 keys in LDS
 template <int DH>
 struct FwdRows {
@@ -154,7 +123,10 @@ struct FwdRows {
       }
     }
   }
-  // whether a result is infinite or NaN, which rows hidden from it may have brought in
+  __device__ __forceinline__ void add_careful(lds_char_ptr sV, const f32x16* s, int k0) {
+    add_with_care<DH>(accO, s, sV, [&](int dt, int) { return ((dt & 1) ? v_off1 : v_off0) + (dt >> 1) * 128; }, own.lo - k0, own.hi - k0);
+  }
+  // whether a result is infinite or NaN, which rows hidden from it may have brought in: then the block is done once more, with care
   __device__ __forceinline__ bool odd() const {
     bool r_ = false;
 #pragma unroll
@@ -183,17 +155,20 @@ struct FwdRows {
   }
 };
 
-// One workgroup's block of rows and heads.  False, and nothing stored: a result is infinite or NaN, which hidden rows may have
-// brought in (never so with CAREFUL).  smem: two buffers of (K tile | V tile); s_span: two ints.
 struct FwdGrid {
   int32_t heads, groups, blocks, log_rows;   // of a workgroup; of the call; of rows; rows of a block
   int32_t at_once;                             // whether all workgroups start at the same time
   float scale_log2e;
 };
-template <int DH, int KG, bool CAREFUL>
-__device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* out, float* lse, const FwdGrid& grid, char* smem, int* s_span) {
+// A workgroup's block of rows and heads: four waves share K/V tiles.  KG = 2: twice four, the second four with every other tile, so
+// that a block's own chain over the keys is half as long; their sums meet in LDS.
+template <int DH, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
   constexpr int NW = 4, TILE = 64 * DH * 2, BUF = KG * 2 * TILE, DT = DH / 32, LD = DH + 4;
-  static_assert(NW * 2048 <= 2 * TILE && (KG == 1 || NW * 32 * LD * 4 <= 2 * BUF), "the second buffers hold a careful wave's probabilities, all of them O of one part");
+  static_assert(KG == 1 || NW * 32 * LD * 4 <= 2 * BUF, "O of one part fits the buffers");
+  extern __shared__ __align__(16) char smem[];   // two buffers of KG (K tile | V tile)
+  __shared__ int s_span[2];
+  __shared__ float s_ml[KG > 1 ? NW : 1][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) % NW, part = __builtin_amdgcn_readfirstlane(tid >> 6) / NW;
   // head groups fastest: workgroups with the same rows run at the same time
   const int hg = (int)(blockIdx.x % (uint32_t)grid.groups);
@@ -228,45 +203,43 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
     copy_k.issue(kh, lds_base + (uint32_t)(buf * BUF), k0, k_end);
     copy_v.issue(vh, lds_base + (uint32_t)(buf * BUF + TILE), k0, k_end);
   };
-  if (!CAREFUL && n_tiles > 0) stage(0, k_begin + part * 64);
-  w.begin();
-  bool fresh = true;
-  for (int kt = part; kt - part < n_tiles; kt += KG) {   // as many steps in every part
-    const int k0 = k_begin + kt * 64, buf = CAREFUL ? 0 : (kt / KG) & 1;
-    if (CAREFUL) {
+  auto walk = [&](auto careful_) {
+    constexpr bool CAREFUL = decltype(careful_)::value;
+    if (n_tiles > 0) stage(0, k_begin + part * 64);
+    w.begin();
+    bool fresh = true;
+    for (int kt = part; kt - part < n_tiles; kt += KG) {   // as many steps in every part
+      const int k0 = k_begin + kt * 64, buf = (kt / KG) & 1;
+      // tile kt has landed (every wave waits for its own copies, then the barrier), and everyone has left the tile before it
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      stage(0, k0);
+      if (k0 + KG * 64 < k_end) stage(buf ^ 1, k0 + KG * 64);
+      if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
+      const char* sK = smem + buf * BUF + part * 2 * TILE;
+      lds_char_ptr sV = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF + part * 2 * TILE;
+      const bool masked = k0 < in_lo || k0 + 64 > in_hi;
+      f32x16 s[2];
+      __builtin_amdgcn_s_setprio(1);   // the other wave of the SIMD fills the gaps
+      w.scores(sK, s);
+      __builtin_amdgcn_s_setprio(0);
+      w.probabilities(sK, s, k0, masked, fresh);
+      fresh = false;
+      if (CAREFUL && masked) {
+        w.add_careful(sV, s, k0);
+        continue;
+      }
+      __builtin_amdgcn_s_setprio(1);
+      w.add(sV, s);
+      __builtin_amdgcn_s_setprio(0);
     }
-    // tile kt has landed (every wave waits for its own copies, then the barrier), and everyone has left the tile before it
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (!CAREFUL && k0 + KG * 64 < k_end) stage(buf ^ 1, k0 + KG * 64);
-    if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
-    const char* sK = smem + buf * BUF + part * 2 * TILE;
-    lds_char_ptr sV = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF + part * 2 * TILE;
-    const bool masked = k0 < in_lo || k0 + 64 > in_hi;
-    f32x16 s[2];
-    __builtin_amdgcn_s_setprio(1);   // the other wave of the SIMD fills the gaps
-    w.scores(sK, s);
-    __builtin_amdgcn_s_setprio(0);
-    w.probabilities(sK, s, k0, masked, fresh);
-    fresh = false;
-    if (CAREFUL && masked) {
-      add_keys<DH>(w.accO, s, sK + TILE, (bf16_t*)(smem + BUF + part * 2 * TILE + wave * 2048), k0, w.own);
-      continue;
-    }
-    __builtin_amdgcn_s_setprio(1);
-    w.add(sV, s);
-    __builtin_amdgcn_s_setprio(0);
-  }
-  if (!CAREFUL) {
-    if (__syncthreads_or(w.odd())) return false;
-  }
+  };
+  walk(std::false_type{});
+  if (__syncthreads_or(w.odd())) walk(std::true_type{});
   w.sum_halves();
   if constexpr (KG == 2) {   // the second part's maximum, sum and O meet the first's
-    if (CAREFUL) __syncthreads();
+    __syncthreads();
     float* sO = (float*)smem + wave * 32 * LD;
-    float* sML = (float*)(s_span + 2) + wave * 64;
+    float* sML = s_ml[wave];
     if (part == 1) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
@@ -280,7 +253,7 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
       }
     }
     __syncthreads();
-    if (part == 1) return true;
+    if (part == 1) return;
     const float m1 = sML[w.lr], m = fmaxf(w.m_ref, m1);
     const float f0 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m_ref - m), f1 = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m1 - m);
     w.l_run = w.l_run * f0 + sML[32 + w.lr] * f1;
@@ -295,20 +268,6 @@ __device__ __forceinline__ bool fwd_block(const PackedQkv<bf16_t>& a, bf16_t* ou
       }
   }
   w.store(a, hd, q_blk + w.lr, out, lse);
-  return true;
-}
-
-// apart from the kernel: its registers are not the kernel's concern
-template <int DH, int KG>
-__device__ __noinline__ void fwd_block_with_care(PackedQkv<bf16_t> a, bf16_t* out, float* lse, FwdGrid grid, char* smem, int* s_span) {
-  fwd_block<DH, KG, true>(a, out, lse, grid, smem, s_span);
-}
-
-template <int DH, int KG>
-__global__ __launch_bounds__(256 * KG, 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
-  extern __shared__ __align__(16) char dyn_smem[];   // two buffers of KG (K tile | V tile)
-  __shared__ int s_span[2 + (KG > 1 ? 256 : 0)];
-  if (!fwd_block<DH, KG, false>(a, out, lse, grid, dyn_smem, s_span)) fwd_block_with_care<DH, KG>(a, out, lse, grid, dyn_smem, s_span);
 }
 
 // Independent waves: each has 32 rows of one head and K/V buffers of its own, so nothing waits for another wave.  KG waves share
@@ -319,7 +278,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_fwd_units_kernel
                                                                                  float* __restrict__ lse, int32_t blocks, int64_t units,
                                                                                  int32_t at_once, float scale_log2e) {
   constexpr int DT = DH / 32, TILE = 64 * DH * 2, NI = TILE / 1024, UNITS = 4 / KG, LD = DH + 4, CPR = DH / 8;
-  constexpr int OWN = 2 * TILE + 2048;   // K tile | V tile | probabilities of a careful wave; later O
+  constexpr int OWN = 2 * TILE + 2048;   // K tile | V tile; later O
   static_assert(32 * LD * 4 <= OWN, "O of a wave fits its buffers");
   extern __shared__ __align__(16) char dyn_smem[];
   __shared__ float sM[4][32], sL[4][32];
@@ -372,7 +331,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_fwd_units_kernel
       } else {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
-      if (CAREFUL && masked) add_keys<DH>(w.accO, s, mine + TILE, (bf16_t*)(mine + 2 * TILE), k0, w.own);
+      if (CAREFUL && masked) w.add_careful(sV, s, k0);
       else w.add(sV, s);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       if (more) copy_v.issue(vh, lds_base + TILE, k0 + KG * 64, k_end);
@@ -462,7 +421,7 @@ int fwd_form(const PackedAttn& a) {
 }  // namespace
 
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
-  int form = fwd_form(a);
+  int form = fwd_form(a); // PF_EXP
   if (a.dh == 64) {
     switch (form) {
       case 1: return launch_units<64, 1>(a, o, out, lse, st);
