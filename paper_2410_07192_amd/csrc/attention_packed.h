@@ -178,12 +178,21 @@ __device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
   hi = __builtin_bit_cast(float, b);
 }
 
+// rows 16 i .. 16 i + 15 of a product's column as a "B" operand: slot (g, t) is row 16 i + 8 (t / 4) + 4 g + t % 4, which is register
+// 8 (i % 2) + t of the product's 32-row half i / 2
+__device__ __forceinline__ bf16x8 as_operand(const f32x16& half, int i) {
+  bf16x8 f;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) f[t] = (__bf16)half[8 * (i & 1) + t];
+  return f;
+}
+
 // acc[dt] += X^T W for a tile that not every row sees as a whole, with care: 0 (hidden) times an infinity or NaN of X would be
 // NaN, so those go into the product as 0 and are counted apart, over visible rows only: a row of X that is +inf, -inf or NaN
-// counts 1, 2^7 or 2^14 (at most 64 rows: exact in fp32).  w: 64 rows of weights as the products left them, visible ones lo .. hi - 1
+// counts 1, 2^7 or 2^14 (at most 64 rows: exact in fp32).  w: the "B" operands of the 64 rows' weights, visible rows lo .. hi - 1
 // (of the tile); off(dt, r): byte offsets of the two transposing reads.  Weights of visible rows are > 0, or NaN, or of either sign with a result that is NaN anyway.
 template <int DH, class Off>
-__device__ __forceinline__ void add_with_care(f32x16* acc, const f32x16* w, lds_char_ptr tile, Off off, int lo, int hi) {
+__device__ __forceinline__ void add_with_care(f32x16* acc, const bf16x8* w, lds_char_ptr tile, Off off, int lo, int hi) {
   const int g = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int dt = 0; dt < DH / 32; ++dt) {
@@ -192,10 +201,9 @@ __device__ __forceinline__ void add_with_care(f32x16* acc, const f32x16* w, lds_
     for (int r = 0; r < 16; ++r) odd[r] = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      asm volatile("" ::: "memory");   // one step's registers at a time
+      __builtin_amdgcn_sched_barrier(0);   // one step's registers at a time
       const v8s x = __builtin_bit_cast(v8s, read_tr<DH * 2>(tile, off(dt, 0), off(dt, 1), i));
       v8s clean, mark, seen;
-      bf16x8 fw;
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         const int row = 16 * i + 8 * (t >> 2) + 4 * g + (t & 3);
@@ -203,9 +211,8 @@ __device__ __forceinline__ void add_with_care(f32x16* acc, const f32x16* w, lds_
         clean[t] = is_odd ? (short)0 : x[t];
         mark[t] = !is_odd ? (short)0 : (x[t] & 0x7f) ? (short)0x4680 : x[t] < 0 ? (short)0x4300 : (short)0x3f80;   // 2^14, 2^7, 1
         seen[t] = row >= lo && row < hi ? (short)0x3f80 : (short)0;
-        fw[t] = (__bf16)w[i >> 1][8 * (i & 1) + t];
       }
-      acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, clean), fw, acc[dt], 0, 0, 0);
+      acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, clean), w[i], acc[dt], 0, 0, 0);
       odd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, seen), odd, 0, 0, 0);
     }
 #pragma unroll

@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_ker
       lds_char_ptr tdO = tQ + TILE;
       const bool masked = q_now < in_lo || q_now + 64 > in_hi;
       const int lo = own.lo - q_now, hi = own.hi - q_now;
-      f32x16 P[2], dS[2];
+      bf16x8 fp[4], fds[4];   // P and dS, rounded to bf16 (half a step, 2^-8 of each)
 #pragma unroll
       for (int qs = 0; qs < 2; ++qs) {
         f32x16 aS, aP;
@@ -172,40 +172,34 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_ker
           const f32x4 L4 = *(const f32x4*)(sL + qi), D4 = *(const f32x4*)(sL + 64 + qi);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(aS[rg * 4 + j], a.scale_log2e, -L4[j]));
-            P[qs][rg * 4 + j] = p;
-            dS[qs][rg * 4 + j] = p * (aP[rg * 4 + j] - D4[j]);
+            const int r = rg * 4 + j;
+            aS[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, -L4[j]));
+            aP[r] = aS[r] * (aP[r] - D4[j]);
           }
         }
         if (masked) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int q = qs * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-            if (q < lo || q >= hi) P[qs][r] = dS[qs][r] = 0.f;
+            if (q < lo || q >= hi) aS[r] = aP[r] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int i = 2 * qs; i < 2 * qs + 2; ++i) {
+          fp[i] = as_operand(aS, i);
+          fds[i] = as_operand(aP, i);
+          if (CAREFUL && masked) continue;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp[i], accV[dt], 0, 0, 0);
+            accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds[i], accK[dt], 0, 0, 0);
           }
         }
       }
       if (CAREFUL && masked) {
         auto off = [&](int dt, int r) { return t_off[dt][r]; };
-        add_with_care<DH>(accV, P, tdO, off, lo, hi);
-        add_with_care<DH>(accK, dS, tQ, off, lo, hi);
-        continue;
-      }
-      // contraction over the 64 queries: K step i covers queries 16 i .. 16 i + 15, operand slot (g, t) is query
-      // 16 i + 8 (t / 4) + 4 g + t % 4 = register 8 (i % 2) + t of sub-tile i / 2
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x8 fp, fds;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          fp[t] = (__bf16)P[i >> 1][8 * (i & 1) + t];
-          fds[t] = (__bf16)dS[i >> 1][8 * (i & 1) + t];
-        }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp, accV[dt], 0, 0, 0);
-          accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds, accK[dt], 0, 0, 0);
-        }
+        add_with_care<DH>(accV, fp, tdO, off, lo, hi);
+        add_with_care<DH>(accK, fds, tQ, off, lo, hi);
       }
     }
   };
@@ -335,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
       lds_char_ptr tK = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
       const bool masked = k0 < in_lo || k0 + 64 > in_hi;
       const int lo = own.lo - k0, hi = own.hi - k0;
-      f32x16 dS[2];
+      bf16x8 fds[4];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         f32x16 aS, aP;
@@ -348,28 +342,24 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
           aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sV + r * ROWB + ((c ^ swz_row<DH>(r)) << 4))), fd[kk], aP, 0, 0, 0);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dS[ks][r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
+        for (int r = 0; r < 16; ++r) aP[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
         if (masked) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = ks * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-            if (key < lo || key >= hi) dS[ks][r] = 0.f;
+            if (key < lo || key >= hi) aP[r] = 0.f;
           }
         }
-      }
-      if (CAREFUL && masked) {
-        add_with_care<DH>(acc, dS, tK, [&](int dt, int r) { return t_off[dt][r]; }, lo, hi);
-        continue;
-      }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x8 fds;
+        for (int i = 2 * ks; i < 2 * ks + 2; ++i) {
+          fds[i] = as_operand(aP, i);
+          if (CAREFUL && masked) continue;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) fds[t] = (__bf16)dS[i >> 1][8 * (i & 1) + t];
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tK, t_off[dt][0], t_off[dt][1], i), fds, acc[dt], 0, 0, 0);
+          for (int dt = 0; dt < DT; ++dt)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tK, t_off[dt][0], t_off[dt][1], i), fds[i], acc[dt], 0, 0, 0);
+        }
       }
+      if (CAREFUL && masked) add_with_care<DH>(acc, fds, tK, [&](int dt, int r) { return t_off[dt][r]; }, lo, hi);
     }
   };
   walk(std::false_type{});

@@ -108,23 +108,22 @@ struct FwdRows {
     m_ref = m_new;
     l_run += exponentials(s);
   }
-  // O^T += V^T P^T: K step i covers keys 16 i .. 16 i + 15, operand slot (g, t) is key 16 i + 8 (t / 4) + 4 g + t % 4 =
-  // register 8 (i % 2) + t of sub-tile i / 2.  P is rounded to bf16 (half a step, 2^-8 of each), its sum is not.
+  // O^T += V^T P^T.  P is rounded to bf16 (half a step, 2^-8 of each), its sum is not.
+  __device__ __forceinline__ int v_off(int dt) const { return ((dt & 1) ? v_off1 : v_off0) + (dt >> 1) * 128; }
   __device__ __forceinline__ void add(lds_char_ptr sV, const f32x16* s) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      bf16x8 fp;
+      const bf16x8 fp = as_operand(s[i >> 1], i);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) fp[t] = (__bf16)s[i >> 1][8 * (i & 1) + t];
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const int off = ((dt & 1) ? v_off1 : v_off0) + (dt >> 1) * 128;
-        accO[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(sV, off, off, i), fp, accO[dt], 0, 0, 0);
-      }
+      for (int dt = 0; dt < DT; ++dt)
+        accO[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(sV, v_off(dt), v_off(dt), i), fp, accO[dt], 0, 0, 0);
     }
   }
   __device__ __forceinline__ void add_careful(lds_char_ptr sV, const f32x16* s, int k0) {
-    add_with_care<DH>(accO, s, sV, [&](int dt, int) { return ((dt & 1) ? v_off1 : v_off0) + (dt >> 1) * 128; }, own.lo - k0, own.hi - k0);
+    bf16x8 fp[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fp[i] = as_operand(s[i >> 1], i);
+    add_with_care<DH>(accO, fp, sV, [&](int dt, int) { return v_off(dt); }, own.lo - k0, own.hi - k0);
   }
   // whether a result is infinite or NaN, which rows hidden from it may have brought in: then the block is done once more, with care
   __device__ __forceinline__ bool odd() const {
