@@ -12,6 +12,10 @@ SOURCES = ["planner.cpp", "scheduler.cpp", "gemm_route.cpp", "gemm_inst_a.hip", 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
+# Kernels with more live values than 256 registers: matrix results stay in vector registers, where the exponentials need them, and only
+# what is left over goes to accumulation registers (otherwise all results go there, and 241 moves a tile bring them back in dK/dV of d_head 128)
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("attention_packed.hip", "attention_packed_fwd.hip", "attention_packed_bwd.hip")}
+
 
 def build(verbose: bool = True, jobs: int = 8) -> str:
     """Compile every source and link the shared library; returns its path."""
@@ -22,7 +26,7 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     for src in SOURCES:
         obj = os.path.join(obj_dir, src + ".o")
         objs.append(obj)
-        cmd = ["hipcc", *FLAGS, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = ["hipcc", *FLAGS, *SOURCE_FLAGS.get(src, []), "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         if len(procs) >= jobs:
             _wait(procs, verbose)

@@ -48,7 +48,7 @@ __device__ __forceinline__ int wave_total(int x) {
 __device__ __forceinline__ int block_in_order(const PackedRows& p, int i, int blocks, int log_rows, int causal, bool from_end, bool at_once) {
   const int plain = causal && from_end ? i : blocks - 1 - i;
   if (at_once || p.start == nullptr || p.n_seq < 2 || p.n_seq > 64) return plain;
-  const int lane = threadIdx.x & 63, up = (1 << log_rows) - 1;
+  const int lane = threadIdx.x & 63, up = from_end ? 0 : (1 << log_rows) - 1;   // a block of two sequences: the one that it meets more rows of
   int b0 = 0, n = 0;
   if (lane < p.n_seq) {   // rows before the first sequence count as its own, rows behind the last as the last's
     b0 = lane == 0 ? 0 : (min(max(p.start[lane], 0), p.tokens) + up) >> log_rows;
@@ -231,7 +231,7 @@ hipError_t allow_lds(const void* kernel, int bytes);
 // bf16, d_head 64 / 128, all pointers 16-byte aligned, strides in eights
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st);
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
-                           void* dv, float* partial, hipStream_t st);
-int64_t packed_bwd_bf16_bytes(const PackedAttn& a);   // of `partial`
+                           void* dv, void* workspace, hipStream_t st);
+int64_t packed_bwd_bf16_bytes(const PackedAttn& a);   // of workspace
 
 }  // namespace pf

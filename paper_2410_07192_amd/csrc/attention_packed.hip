@@ -472,7 +472,7 @@ hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (vec && by_bf16(a))
-    return packed_bwd_bf16(a, operands<bf16_t>(a, q, k, v), dout, lse, dsum, dq, dk, dv, (float*)((char*)workspace + dsum_bytes(a)), st);
+    return packed_bwd_bf16(a, operands<bf16_t>(a, q, k, v), dout, lse, dsum, dq, dk, dv, (char*)workspace + dsum_bytes(a), st);
 #define PF_BWD(T, D, V) bwd<T, D, V>(a, q, k, v, dout, lse, dsum, dq, dk, dv, st)
   PF_BY_SHAPE(PF_BWD);
 #undef PF_BWD

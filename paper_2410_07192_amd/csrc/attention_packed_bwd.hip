@@ -10,11 +10,10 @@
 //    transposing LDS load.  Where keys and K/V heads are too few for the card, the heads of a group are dealt out to several
 //    workgroups, whose fp32 sums a third launch adds up.
 //  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
-// Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h and the forward kernel; here
-// too a result with an infinity or NaN is computed a second time with care.
+// Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h.  A workgroup whose results
+// hold an infinity or NaN, which rows hidden from them may have brought in, leaves a mark, and one more launch does the marked
+// ones again with care.  (As a second walk inside the kernels, as in the forward pass, it cost them registers: spills made dK/dV of d_head 128 twice as slow.)
 #include "attention_packed.h"
-
-#include <type_traits>
 
 namespace pf {
 namespace {
@@ -61,23 +60,26 @@ struct BwdArgs {
   const float *lse, *dsum;
   bf16_t *dq, *dk, *dv;
   float* partial;                              // [split][dK, dV][tokens][K/V heads * d_head], or null with one split
-  int32_t blocks, splits, heads, at_once;      // blocks of rows; parts of a group's heads (dK/dV); heads of a workgroup (dQ)
+  int32_t* marks;                              // of the workgroups of dK/dV, then of dQ
+  int32_t k_blocks, splits;                    // dK/dV: blocks of 128 keys, parts of a group's heads
+  int32_t q_blocks, heads;                     // dQ: blocks of rows, heads of a workgroup
+  int32_t k_units, q_units;                    // workgroups
+  int32_t at_once;                             // they start at the same time: 1 dK/dV, 2 dQ
   float scale_log2e;
 };
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------------
-template <int DH>
-__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_kernel(BwdArgs a) {
+// Workgroup `unit`; whether a result is infinite or NaN.  smem: two buffers; s_span: two ints.
+template <int DH, bool CAREFUL>
+__device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB;
   constexpr int BUF = 2 * TILE + 512;   // Q tile | dO tile | lse (log2 units) of the 64 queries | D
-  extern __shared__ __align__(16) char smem[];   // two buffers
-  __shared__ int s_span[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
   const int n_kv = a.o.h / a.o.group, T = a.o.rows.tokens;
   // K/V heads and splits fastest: workgroups with the same rows run at the same time
   const uint32_t per = (uint32_t)(n_kv * a.splits);
-  const int hk = (int)(blockIdx.x % per) % n_kv, split = (int)(blockIdx.x % per) / n_kv;
-  const int k_blk = block_in_order(a.o.rows, (int)(blockIdx.x / per), a.blocks, 7, a.o.causal, true, a.at_once) * 128;
+  const int hk = (int)((uint32_t)unit % per) % n_kv, split = (int)((uint32_t)unit % per) / n_kv;
+  const int k_blk = block_in_order(a.o.rows, (int)((uint32_t)unit / per), a.k_blocks, 7, a.o.causal, true, a.at_once & 1) * 128;
   const int key = k_blk + wave * 32 + lr;
   bf16x8 fk[KS], fv[KS];
   {
@@ -119,93 +121,89 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_ker
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fk[kk]), "v"(fv[kk]));   // waited for here, once
   const int steps = tiles * (h1 - h0);
-  auto walk = [&](auto careful_) {
-    constexpr bool CAREFUL = decltype(careful_)::value;
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+  for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
-    float ld = 0.f;
-    int hd = h0, q0 = q_begin;
-    if (steps > 0) {
-      stage(0, hd, q0);
+    for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
+  float ld = 0.f;
+  int hd = h0, q0 = q_begin;
+  if (steps > 0) {
+    stage(0, hd, q0);
+    ld = load_ld(hd, q0);
+  }
+  for (int it = 0; it < steps; ++it) {
+    const int buf = it & 1, q_now = q0;
+    write_ld(buf, ld);   // the buffer was last read before the barrier of the previous step
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    q0 += 64;
+    if (q0 >= q_end) {
+      q0 = q_begin;
+      ++hd;
+    }
+    if (it + 1 < steps) {
+      stage(buf ^ 1, hd, q0);
       ld = load_ld(hd, q0);
     }
-    for (int it = 0; it < steps; ++it) {
-      const int buf = it & 1, q_now = q0;
-      write_ld(buf, ld);   // the buffer was last read before the barrier of the previous step
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      q0 += 64;
-      if (q0 >= q_end) {
-        q0 = q_begin;
-        ++hd;
+    if (q_now + 64 <= w_lo || q_now >= w_hi) continue;   // none of the wave's keys is seen from the tile
+    const char* sQ = smem + buf * BUF;
+    const char* sdO = sQ + TILE;
+    const float* sL = (const float*)(sQ + 2 * TILE);
+    lds_char_ptr tQ = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
+    lds_char_ptr tdO = tQ + TILE;
+    const bool masked = q_now < in_lo || q_now + 64 > in_hi;
+    const int lo = own.lo - q_now, hi = own.hi - q_now;
+    bf16x8 fp[4], fds[4];   // P and dS, rounded to bf16 (half a step, 2^-8 of each)
+#pragma unroll
+    for (int qs = 0; qs < 2; ++qs) {
+      f32x16 aS, aP;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const int r = qs * 32 + lr;
+        const int o = r * ROWB + (((kk * 2 + g) ^ SwzBoth<DH>::of(r)) << 4);
+        aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sQ + o)), fk[kk], aS, 0, 0, 0);
+        aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
       }
-      if (it + 1 < steps) {
-        stage(buf ^ 1, hd, q0);
-        ld = load_ld(hd, q0);
-      }
-      if (q_now + 64 <= w_lo || q_now >= w_hi) continue;   // none of the wave's keys is seen from the tile
-      const char* sQ = smem + buf * BUF;
-      const char* sdO = sQ + TILE;
-      const float* sL = (const float*)(sQ + 2 * TILE);
-      lds_char_ptr tQ = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
-      lds_char_ptr tdO = tQ + TILE;
-      const bool masked = q_now < in_lo || q_now + 64 > in_hi;
-      const int lo = own.lo - q_now, hi = own.hi - q_now;
-      bf16x8 fp[4], fds[4];   // P and dS, rounded to bf16 (half a step, 2^-8 of each)
 #pragma unroll
-      for (int qs = 0; qs < 2; ++qs) {
-        f32x16 aS, aP;
+      for (int rg = 0; rg < 4; ++rg) {
+        const int qi = qs * 32 + 8 * rg + 4 * g;
+        const f32x4 L4 = *(const f32x4*)(sL + qi), D4 = *(const f32x4*)(sL + 64 + qi);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          const int r = qs * 32 + lr;
-          const int o = r * ROWB + (((kk * 2 + g) ^ SwzBoth<DH>::of(r)) << 4);
-          aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sQ + o)), fk[kk], aS, 0, 0, 0);
-          aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
-        }
-#pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-          const int qi = qs * 32 + 8 * rg + 4 * g;
-          const f32x4 L4 = *(const f32x4*)(sL + qi), D4 = *(const f32x4*)(sL + 64 + qi);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = rg * 4 + j;
-            aS[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, -L4[j]));
-            aP[r] = aS[r] * (aP[r] - D4[j]);
-          }
-        }
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int q = qs * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-            if (q < lo || q >= hi) aS[r] = aP[r] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int i = 2 * qs; i < 2 * qs + 2; ++i) {
-          fp[i] = as_operand(aS, i);
-          fds[i] = as_operand(aP, i);
-          if (CAREFUL && masked) continue;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp[i], accV[dt], 0, 0, 0);
-            accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds[i], accK[dt], 0, 0, 0);
-          }
+        for (int j = 0; j < 4; ++j) {
+          const int r = rg * 4 + j;
+          aS[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, -L4[j]));
+          aP[r] = aS[r] * (aP[r] - D4[j]);
         }
       }
-      if (CAREFUL && masked) {
-        auto off = [&](int dt, int r) { return t_off[dt][r]; };
-        add_with_care<DH>(accV, fp, tdO, off, lo, hi);
-        add_with_care<DH>(accK, fds, tQ, off, lo, hi);
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int q = qs * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+          if (q < lo || q >= hi) aS[r] = aP[r] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 2 * qs; i < 2 * qs + 2; ++i) {
+        fp[i] = as_operand(aS, i);
+        fds[i] = as_operand(aP, i);
+        if (CAREFUL && masked) continue;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp[i], accV[dt], 0, 0, 0);
+          accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds[i], accK[dt], 0, 0, 0);
+        }
       }
     }
-  };
-  walk(std::false_type{});
-  if (__syncthreads_or((not_finite<DT>(accK) || not_finite<DT>(accV)) && own.lo < own.hi)) walk(std::true_type{});
-  if (own.lo >= own.hi) return;
+    if (CAREFUL && masked) {
+      auto off = [&](int dt, int r) { return t_off[dt][r]; };
+      add_with_care<DH>(accV, fp, tdO, off, lo, hi);
+      add_with_care<DH>(accK, fds, tQ, off, lo, hi);
+    }
+  }
+  const bool odd = !CAREFUL && __syncthreads_or((not_finite<DT>(accK) || not_finite<DT>(accV)) && own.lo < own.hi);
+  if (own.lo >= own.hi) return odd;
   if (a.partial == nullptr) {
     bf16_t* pk = a.dk + (int64_t)key * a.o.ld_k + hk * DH;
     bf16_t* pv = a.dv + (int64_t)key * a.o.ld_v + hk * DH;
@@ -233,6 +231,15 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_ker
         *(f32x4*)(pv + dt * 32 + rg * 8 + g * 4) = f32x4{accV[dt][rg * 4], accV[dt][rg * 4 + 1], accV[dt][rg * 4 + 2], accV[dt][rg * 4 + 3]};
       }
   }
+  return odd;
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_kernel(BwdArgs a) {
+  extern __shared__ __align__(16) char dyn_smem[];
+  __shared__ int s_span[2];
+  const bool odd = dkv_block<DH, false>(a, (int)blockIdx.x, dyn_smem, s_span);
+  if (threadIdx.x == 0) a.marks[blockIdx.x] = odd;
 }
 
 // dK, dV from the splits' sums: eight columns a thread, rows that are in a sequence
@@ -263,15 +270,13 @@ __global__ __launch_bounds__(256) void packed_bwd_join_kernel(BwdArgs a) {
 }
 
 // ---- dQ ----------------------------------------------------------------------------------------------------------------------
-template <int DH>
-__global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
-  extern __shared__ __align__(16) char smem[];   // two buffers
-  __shared__ int s_span[2];
+template <int DH, bool CAREFUL>
+__device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB, BUF = 2 * TILE;   // K tile | V tile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
   const int T = a.o.rows.tokens, groups = a.o.h / a.heads, tiles_of_rows = 4 / a.heads;
-  const int hg = (int)(blockIdx.x % (uint32_t)groups);
-  const int blk = block_in_order(a.o.rows, (int)(blockIdx.x / (uint32_t)groups), a.blocks, 5 + (tiles_of_rows >> 1), a.o.causal, false, a.at_once);
+  const int hg = (int)((uint32_t)unit % (uint32_t)groups);
+  const int blk = block_in_order(a.o.rows, (int)((uint32_t)unit / (uint32_t)groups), a.q_blocks, 5 + (tiles_of_rows >> 1), a.o.causal, false, a.at_once & 2);
   const int hd = hg * a.heads + wave % a.heads, q_blk = (blk * tiles_of_rows + wave / a.heads) * 32;
   const int q_row = q_blk + lr, q_cl = min(q_row, T - 1);
   bf16x8 fq[KS], fd[KS];
@@ -311,60 +316,56 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fq[kk]), "v"(fd[kk]));   // waited for here, once
   asm volatile("" ::"v"(neg_l), "v"(D));
-  auto walk = [&](auto careful_) {
-    constexpr bool CAREFUL = decltype(careful_)::value;
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+  for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
-    if (n_tiles > 0) stage(0, k_begin);
-    for (int kt = 0; kt < n_tiles; ++kt) {
-      const int k0 = k_begin + kt * 64, buf = kt & 1;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (kt + 1 < n_tiles) stage(buf ^ 1, k0 + 64);
-      if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
-      const char* sK = smem + buf * BUF;
-      const char* sV = sK + TILE;
-      lds_char_ptr tK = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
-      const bool masked = k0 < in_lo || k0 + 64 > in_hi;
-      const int lo = own.lo - k0, hi = own.hi - k0;
-      bf16x8 fds[4];
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+  if (n_tiles > 0) stage(0, k_begin);
+  for (int kt = 0; kt < n_tiles; ++kt) {
+    const int k0 = k_begin + kt * 64, buf = kt & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (kt + 1 < n_tiles) stage(buf ^ 1, k0 + 64);
+    if (k0 + 64 <= w_lo || k0 >= w_hi) continue;   // none of the wave's rows sees the tile
+    const char* sK = smem + buf * BUF;
+    const char* sV = sK + TILE;
+    lds_char_ptr tK = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
+    const bool masked = k0 < in_lo || k0 + 64 > in_hi;
+    const int lo = own.lo - k0, hi = own.hi - k0;
+    bf16x8 fds[4];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        f32x16 aS, aP;
+    for (int ks = 0; ks < 2; ++ks) {
+      f32x16 aS, aP;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+      for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          const int r = ks * 32 + lr, c = kk * 2 + g;
-          aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sK + r * ROWB + ((c ^ SwzBoth<DH>::of(r)) << 4))), fq[kk], aS, 0, 0, 0);
-          aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sV + r * ROWB + ((c ^ swz_row<DH>(r)) << 4))), fd[kk], aP, 0, 0, 0);
-        }
+      for (int kk = 0; kk < KS; ++kk) {
+        const int r = ks * 32 + lr, c = kk * 2 + g;
+        aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sK + r * ROWB + ((c ^ SwzBoth<DH>::of(r)) << 4))), fq[kk], aS, 0, 0, 0);
+        aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sV + r * ROWB + ((c ^ swz_row<DH>(r)) << 4))), fd[kk], aP, 0, 0, 0);
+      }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) aP[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
-        if (masked) {
+      for (int r = 0; r < 16; ++r) aP[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
+      if (masked) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = ks * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-            if (key < lo || key >= hi) aP[r] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int i = 2 * ks; i < 2 * ks + 2; ++i) {
-          fds[i] = as_operand(aP, i);
-          if (CAREFUL && masked) continue;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tK, t_off[dt][0], t_off[dt][1], i), fds[i], acc[dt], 0, 0, 0);
+        for (int r = 0; r < 16; ++r) {
+          const int key = ks * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
+          if (key < lo || key >= hi) aP[r] = 0.f;
         }
       }
-      if (CAREFUL && masked) add_with_care<DH>(acc, fds, tK, [&](int dt, int r) { return t_off[dt][r]; }, lo, hi);
+#pragma unroll
+      for (int i = 2 * ks; i < 2 * ks + 2; ++i) {
+        fds[i] = as_operand(aP, i);
+        if (CAREFUL && masked) continue;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tK, t_off[dt][0], t_off[dt][1], i), fds[i], acc[dt], 0, 0, 0);
+      }
     }
-  };
-  walk(std::false_type{});
-  if (__syncthreads_or(not_finite<DT>(acc) && own.lo < own.hi)) walk(std::true_type{});
-  if (own.lo >= own.hi) return;
+    if (CAREFUL && masked) add_with_care<DH>(acc, fds, tK, [&](int dt, int r) { return t_off[dt][r]; }, lo, hi);
+  }
+  const bool odd = !CAREFUL && __syncthreads_or(not_finite<DT>(acc) && own.lo < own.hi);
+  if (own.lo >= own.hi) return odd;
   bf16_t* row = a.dq + (int64_t)q_row * a.o.ld_q + hd * DH;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -375,6 +376,34 @@ __global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
       for (int j = 0; j < 4; ++j) v[j] = acc[dt][rg * 4 + j] * a.o.scale;
       store4(row + dt * 32 + rg * 8 + g * 4, v);
     }
+  return odd;
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
+  extern __shared__ __align__(16) char dyn_smem[];
+  __shared__ int s_span[2];
+  const bool odd = dq_block<DH, false>(a, (int)blockIdx.x, dyn_smem, s_span);
+  if (threadIdx.x == 0) a.marks[a.k_units + blockIdx.x] = odd;
+}
+
+// The marked workgroups' results again, with care
+template <int DH>
+__global__ __launch_bounds__(256, 1) void packed_bwd_again_kernel(BwdArgs a) {
+  extern __shared__ __align__(16) char dyn_smem[];
+  __shared__ int s_span[2];
+  const int lane = threadIdx.x & 63, n = a.k_units + a.q_units, step = gridDim.x;
+  for (int u0 = blockIdx.x; u0 < n; u0 += 64 * step) {
+    const int64_t u = u0 + (int64_t)lane * step;
+    uint64_t left = __ballot(u < n && a.marks[u < n ? u : 0] != 0);   // the same in every wave
+    while (left) {
+      const int unit = u0 + (__ffsll((unsigned long long)left) - 1) * step;
+      left &= left - 1;
+      __syncthreads();
+      if (unit < a.k_units) dkv_block<DH, true>(a, unit, dyn_smem, s_span);
+      else dq_block<DH, true>(a, unit - a.k_units, dyn_smem, s_span);
+    }
+  }
 }
 
 // parts of a group's heads in dK/dV: as many as give every CU two workgroups
@@ -386,38 +415,56 @@ int splits_of(const PackedAttn& a) {
   return s;
 }
 
-template <int DH>
-hipError_t run(const PackedAttn& a, BwdArgs b, hipStream_t st) {
-  constexpr int lds_dkv = 2 * (2 * 64 * DH * 2 + 512), lds_dq = 2 * 2 * 64 * DH * 2;
-  hipError_t e = allow_lds((const void*)packed_bwd_dkv_bf16_kernel<DH>, lds_dkv);
-  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_dq_bf16_kernel<DH>, lds_dq);
-  if (e != hipSuccess) return e;
-  b.blocks = (int32_t)((a.tokens + 127) / 128);
-  int64_t grid = (int64_t)b.blocks * a.h_kv * b.splits;
-  b.at_once = grid <= (DH == 64 ? 512 : 256);
-  hipLaunchKernelGGL(packed_bwd_dkv_bf16_kernel<DH>, dim3((unsigned)grid), dim3(256), lds_dkv, st, b);
-  if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
+// how the work is divided: a function of the sizes alone
+BwdArgs plan_of(const PackedAttn& a) {
+  BwdArgs b{};
+  b.k_blocks = (int32_t)((a.tokens + 127) / 128);
+  b.splits = splits_of(a);
+  b.k_units = b.k_blocks * a.h_kv * b.splits;
   b.heads = 1;
   while (b.heads < 4 && (a.h / a.h_kv) % (b.heads * 2) == 0) b.heads *= 2;
   const int rows = 128 / b.heads;
-  b.blocks = (int32_t)((a.tokens + rows - 1) / rows);
-  grid = (int64_t)b.blocks * (a.h / b.heads);
-  b.at_once = grid <= 512;
-  hipLaunchKernelGGL(packed_bwd_dq_bf16_kernel<DH>, dim3((unsigned)grid), dim3(256), lds_dq, st, b);
+  b.q_blocks = (int32_t)((a.tokens + rows - 1) / rows);
+  b.q_units = b.q_blocks * (a.h / b.heads);
+  b.at_once = (b.k_units <= (a.dh == 64 ? 512 : 256) ? 1 : 0) | (b.q_units <= 512 ? 2 : 0);
+  return b;
+}
+int64_t marks_bytes(const BwdArgs& b) { return ((int64_t)b.k_units + b.q_units + 63) / 64 * 256; }
+
+template <int DH>
+hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
+  constexpr int lds_dkv = 2 * (2 * 64 * DH * 2 + 512), lds_dq = 2 * 2 * 64 * DH * 2;
+  hipError_t e = allow_lds((const void*)packed_bwd_dkv_bf16_kernel<DH>, lds_dkv);
+  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_dq_bf16_kernel<DH>, lds_dq);
+  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_again_kernel<DH>, lds_dkv);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(packed_bwd_dkv_bf16_kernel<DH>, dim3((unsigned)b.k_units), dim3(256), lds_dkv, st, b);
+  hipLaunchKernelGGL(packed_bwd_dq_bf16_kernel<DH>, dim3((unsigned)b.q_units), dim3(256), lds_dq, st, b);
+  hipLaunchKernelGGL(packed_bwd_again_kernel<DH>, dim3((unsigned)(b.k_units + b.q_units < 256 ? b.k_units + b.q_units : 256)), dim3(256), lds_dkv, st, b);
+  if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t packed_bwd_bf16_bytes(const PackedAttn& a) {
-  const int s = splits_of(a);
-  return s > 1 ? (int64_t)s * 2 * a.tokens * a.h_kv * a.dh * 4 : 0;
+  const BwdArgs b = plan_of(a);
+  return marks_bytes(b) + (b.splits > 1 ? (int64_t)b.splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0);
 }
 
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
-                           void* dv, float* partial, hipStream_t st) {
-  BwdArgs b{o, (const bf16_t*)dout, lse, dsum, (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, nullptr, 0, splits_of(a), 0, 0, LOG2E_P * o.scale};
-  if (b.splits > 1) b.partial = partial;
+                           void* dv, void* workspace, hipStream_t st) {
+  BwdArgs b = plan_of(a);
+  b.o = o;
+  b.dout = (const bf16_t*)dout;
+  b.lse = lse;
+  b.dsum = dsum;
+  b.dq = (bf16_t*)dq;
+  b.dk = (bf16_t*)dk;
+  b.dv = (bf16_t*)dv;
+  b.marks = (int32_t*)workspace;
+  b.partial = b.splits > 1 ? (float*)((char*)workspace + marks_bytes(b)) : nullptr;
+  b.scale_log2e = LOG2E_P * o.scale;
   return a.dh == 64 ? run<64>(a, b, st) : run<128>(a, b, st);
 }
 
