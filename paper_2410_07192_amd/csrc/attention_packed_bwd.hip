@@ -11,8 +11,8 @@
 //    workgroups, whose fp32 sums a third launch adds up.
 //  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
 // Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h.  A workgroup whose results
-// hold an infinity or NaN, which rows hidden from them may have brought in, leaves a mark, and one more launch does the marked
-// ones again with care.  (As a second walk inside the kernels, as in the forward pass, it cost them registers: spills made dK/dV of d_head 128 twice as slow.)
+// hold an infinity or NaN, which rows hidden from them may have brought in, does them again with care; where the two passes are
+// launches of their own (d_head 128, large) it leaves a mark and a last launch does so, for the registers' sake.
 #include "attention_packed.h"
 
 namespace pf {
@@ -234,14 +234,6 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   return odd;
 }
 
-template <int DH>
-__global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_bwd_dkv_bf16_kernel(BwdArgs a) {
-  extern __shared__ __align__(16) char dyn_smem[];
-  __shared__ int s_span[2];
-  const bool odd = dkv_block<DH, false>(a, (int)blockIdx.x, dyn_smem, s_span);
-  if (threadIdx.x == 0) a.marks[blockIdx.x] = odd;
-}
-
 // dK, dV from the splits' sums: eight columns a thread, rows that are in a sequence
 template <int DH>
 __global__ __launch_bounds__(256) void packed_bwd_join_kernel(BwdArgs a) {
@@ -379,12 +371,24 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
   return odd;
 }
 
-template <int DH>
-__global__ __launch_bounds__(256, 2) void packed_bwd_dq_bf16_kernel(BwdArgs a) {
+// Both passes in one launch (WHAT 3: the dK/dV workgroups first, they are the longer ones), so that few workgroups of one do not leave
+// the card idle; or one of them (1 dK/dV, 2 dQ), which leaves marks.
+template <int DH, int WHAT>
+__global__ __launch_bounds__(256, DH == 64 || WHAT == 2 ? 2 : 1) void packed_bwd_bf16_kernel(BwdArgs a) {
   extern __shared__ __align__(16) char dyn_smem[];
   __shared__ int s_span[2];
-  const bool odd = dq_block<DH, false>(a, (int)blockIdx.x, dyn_smem, s_span);
-  if (threadIdx.x == 0) a.marks[a.k_units + blockIdx.x] = odd;
+  const int unit = (int)blockIdx.x + (WHAT == 2 ? a.k_units : 0);
+  const bool is_k = WHAT == 1 || (WHAT == 3 && unit < a.k_units);
+  bool odd;
+  if (is_k) odd = dkv_block<DH, false>(a, unit, dyn_smem, s_span);
+  else odd = dq_block<DH, false>(a, unit - a.k_units, dyn_smem, s_span);
+  if (WHAT != 3) {
+    if (threadIdx.x == 0) a.marks[unit] = odd;
+  } else if (odd) {
+    __syncthreads();
+    if (is_k) dkv_block<DH, true>(a, unit, dyn_smem, s_span);
+    else dq_block<DH, true>(a, unit - a.k_units, dyn_smem, s_span);
+  }
 }
 
 // The marked workgroups' results again, with care
@@ -429,18 +433,34 @@ BwdArgs plan_of(const PackedAttn& a) {
   b.at_once = (b.k_units <= (a.dh == 64 ? 512 : 256) ? 1 : 0) | (b.q_units <= 512 ? 2 : 0);
   return b;
 }
+// Whether both passes are one launch.  d_head 64: always, they use as many registers.  d_head 128: dQ then runs with one wave per SIMD as
+// dK/dV does, not two (24 / 8 heads, 6600 rows: 297 us apart, 311 together; 18 / 6 heads, 150 rows: 36 and 25)
+bool together(const PackedAttn& a, int units) { return a.dh == 64 || units <= 1024; }
 int64_t marks_bytes(const BwdArgs& b) { return ((int64_t)b.k_units + b.q_units + 63) / 64 * 256; }
+
+template <int DH, int WHAT>
+hipError_t launch_passes(const BwdArgs& b, hipStream_t st) {
+  constexpr int lds = WHAT == 2 ? 2 * 2 * 64 * DH * 2 : 2 * (2 * 64 * DH * 2 + 512);
+  hipError_t e = allow_lds((const void*)packed_bwd_bf16_kernel<DH, WHAT>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((packed_bwd_bf16_kernel<DH, WHAT>), dim3((unsigned)((WHAT & 1 ? b.k_units : 0) + (WHAT & 2 ? b.q_units : 0))), dim3(256), lds, st, b);
+  return hipGetLastError();
+}
 
 template <int DH>
 hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
-  constexpr int lds_dkv = 2 * (2 * 64 * DH * 2 + 512), lds_dq = 2 * 2 * 64 * DH * 2;
-  hipError_t e = allow_lds((const void*)packed_bwd_dkv_bf16_kernel<DH>, lds_dkv);
-  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_dq_bf16_kernel<DH>, lds_dq);
-  if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_again_kernel<DH>, lds_dkv);
+  const int units = b.k_units + b.q_units;
+  hipError_t e;
+  if (together(a, units)) {
+    e = launch_passes<DH, 3>(b, st);
+  } else {
+    e = launch_passes<DH, 1>(b, st);
+    if (e == hipSuccess) e = launch_passes<DH, 2>(b, st);
+    constexpr int lds = 2 * (2 * 64 * DH * 2 + 512);
+    if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_again_kernel<DH>, lds);
+    if (e == hipSuccess) hipLaunchKernelGGL(packed_bwd_again_kernel<DH>, dim3((unsigned)(units < 256 ? units : 256)), dim3(256), lds, st, b);
+  }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(packed_bwd_dkv_bf16_kernel<DH>, dim3((unsigned)b.k_units), dim3(256), lds_dkv, st, b);
-  hipLaunchKernelGGL(packed_bwd_dq_bf16_kernel<DH>, dim3((unsigned)b.q_units), dim3(256), lds_dq, st, b);
-  hipLaunchKernelGGL(packed_bwd_again_kernel<DH>, dim3((unsigned)(b.k_units + b.q_units < 256 ? b.k_units + b.q_units : 256)), dim3(256), lds_dkv, st, b);
   if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
   return hipGetLastError();
 }
