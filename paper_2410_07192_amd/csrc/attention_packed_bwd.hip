@@ -7,13 +7,15 @@
 //  * dK/dV: a workgroup has 128 keys of a K/V head, a wave 32 of them with K and V as "B" operands in registers, and walks the
 //    tiles of 64 queries of the group's heads.  S = Q K^T and dP = dO V^T put one key and 32 of a tile's 64 queries into a lane:
 //    the "B" operands of dV^T += dO^T P and dK^T += Q^T dS, whose "A" operands come out of the same row-major tiles by the
-//    transposing LDS load.  Where keys and K/V heads are too few for the card, the heads of a group are dealt out to several
-//    workgroups, whose fp32 sums a third launch adds up.
+//    transposing LDS load.  Where keys and K/V heads are too few for the card, the tiles are dealt out to several workgroups, whose
+//    fp32 sums one more launch adds up.
 //  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
 // Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h.  A workgroup whose results
-// hold an infinity or NaN, which rows hidden from them may have brought in, does them again with care; where the two passes are
-// launches of their own (d_head 128, large) it leaves a mark and a last launch does so, for the registers' sake.
+// hold an infinity or NaN, which rows hidden from them may have brought in, does them again with care, as a second stretch of code behind the first
+// (woven into the first it cost that one registers: dK/dV of d_head 128 took 1880 us instead of 780).
 #include "attention_packed.h"
+
+#include <algorithm>
 
 namespace pf {
 namespace {
@@ -60,8 +62,7 @@ struct BwdArgs {
   const float *lse, *dsum;
   bf16_t *dq, *dk, *dv;
   float* partial;                              // [split][dK, dV][tokens][K/V heads * d_head], or null with one split
-  int32_t* marks;                              // of the workgroups of dK/dV, then of dQ
-  int32_t k_blocks, splits;                    // dK/dV: blocks of 128 keys, parts of a group's heads
+  int32_t k_blocks, splits;                    // dK/dV: blocks of 128 keys, parts of a block's tiles
   int32_t q_blocks, heads;                     // dQ: blocks of rows, heads of a workgroup
   int32_t k_units, q_units;                    // workgroups
   int32_t at_once;                             // they start at the same time: 1 dK/dV, 2 dQ
@@ -100,7 +101,6 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   __syncthreads();
   const int q_begin = __builtin_amdgcn_readfirstlane(s_span[0]), q_end = __builtin_amdgcn_readfirstlane(s_span[1]);
   const int tiles = q_end > q_begin ? (q_end - q_begin + 63) >> 6 : 0;
-  const int h0 = hk * a.o.group + a.o.group * split / a.splits, h1 = hk * a.o.group + a.o.group * (split + 1) / a.splits;
 
   TileCopy<DH, 4, SwzBoth<DH>> copy_q, copy_d;
   copy_q.init(a.o.ld_q, wave);
@@ -120,14 +120,19 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   f32x16 accK[DT], accV[DT];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fk[kk]), "v"(fv[kk]));   // waited for here, once
-  const int steps = tiles * (h1 - h0);
+  // the tiles of one head after the other; this split's part of them
+  const int64_t all = (int64_t)tiles * a.o.group;
+  const int64_t first = all * split / a.splits;
+  const int steps = (int)(all * (split + 1) / a.splits - first);
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
   float ld = 0.f;
-  int hd = h0, q0 = q_begin;
+  int hd = hk * a.o.group, q0 = q_begin;
   if (steps > 0) {
+    hd += (int)(first / tiles);
+    q0 += (int)(first % tiles) * 64;
     stage(0, hd, q0);
     ld = load_ld(hd, q0);
   }
@@ -372,7 +377,7 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 }
 
 // Both passes in one launch (WHAT 3: the dK/dV workgroups first, they are the longer ones), so that few workgroups of one do not leave
-// the card idle; or one of them (1 dK/dV, 2 dQ), which leaves marks.
+// the card idle; or one of them (1 dK/dV, 2 dQ).
 template <int DH, int WHAT>
 __global__ __launch_bounds__(256, DH == 64 || WHAT == 2 ? 2 : 1) void packed_bwd_bf16_kernel(BwdArgs a) {
   extern __shared__ __align__(16) char dyn_smem[];
@@ -382,41 +387,41 @@ __global__ __launch_bounds__(256, DH == 64 || WHAT == 2 ? 2 : 1) void packed_bwd
   bool odd;
   if (is_k) odd = dkv_block<DH, false>(a, unit, dyn_smem, s_span);
   else odd = dq_block<DH, false>(a, unit - a.k_units, dyn_smem, s_span);
-  if (WHAT != 3) {
-    if (threadIdx.x == 0) a.marks[unit] = odd;
-  } else if (odd) {
+  if (odd) {
     __syncthreads();
     if (is_k) dkv_block<DH, true>(a, unit, dyn_smem, s_span);
     else dq_block<DH, true>(a, unit - a.k_units, dyn_smem, s_span);
   }
 }
 
-// The marked workgroups' results again, with care
-template <int DH>
-__global__ __launch_bounds__(256, 1) void packed_bwd_again_kernel(BwdArgs a) {
-  extern __shared__ __align__(16) char dyn_smem[];
-  __shared__ int s_span[2];
-  const int lane = threadIdx.x & 63, n = a.k_units + a.q_units, step = gridDim.x;
-  for (int u0 = blockIdx.x; u0 < n; u0 += 64 * step) {
-    const int64_t u = u0 + (int64_t)lane * step;
-    uint64_t left = __ballot(u < n && a.marks[u < n ? u : 0] != 0);   // the same in every wave
-    while (left) {
-      const int unit = u0 + (__ffsll((unsigned long long)left) - 1) * step;
-      left &= left - 1;
-      __syncthreads();
-      if (unit < a.k_units) dkv_block<DH, true>(a, unit, dyn_smem, s_span);
-      else dq_block<DH, true>(a, unit - a.k_units, dyn_smem, s_span);
-    }
-  }
+// What the host knows of the lengths: how many sequences there are.  Rows that a row meets, on average.
+double rows_met(const PackedAttn& a) {
+  const double length = (double)a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
+  return a.causal ? length / 2 : length;
 }
 
-// parts of a group's heads in dK/dV: as many as give every CU two workgroups
+// Parts of a block's tiles in dK/dV: the number with the least estimated time.  A workgroup takes `start` and `tile` us per tile of 64
+// queries; either the card's `slots` are full, or the longest block's chain counts (its sequence `longest` times the average);
+// with parts, their fp32 sums go through memory at 4 TB/s in `join` us more.  Fitted to 160 drawn sizes with 1 to 12 parts (MI355X):
+// 2.4 % off the best number on average, 24 % at most (one part everywhere: 45 %).  16 heads of 128 on 2 K/V heads, 8969 rows: 1606 us
+// with one part, 660 with four; 12 on 4, 5750 rows: 247 and 157 (two).
 int splits_of(const PackedAttn& a) {
-  const int group = a.h / a.h_kv;
-  const int64_t units = (a.tokens + 127) / 128 * a.h_kv;
-  int s = 1;
-  while (s < group && units * s < 512) ++s;
-  return s;
+  struct Cost { double start, tile, slots, join, longest; };
+  const Cost c = a.dh == 64 ? Cost{3, 1.6, 256, 4, 2.5} : Cost{10, 2.2, 192, 2, 1.5};
+  const double units = (double)((a.tokens + 127) / 128 * a.h_kv), group = (double)(a.h / a.h_kv), length = (double)a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
+  const double most = a.n_seq > 1 ? std::min((double)a.tokens, c.longest * length) : length;
+  const double tiles = group * ((rows_met(a) + 128) / 64 + 0.5), chain = group * ((most + 128) / 64 + 0.5);
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 16 && (s == 1 || s <= 0.75 * tiles); ++s) {
+    const double full = std::max(1.0, units * s / c.slots) * (c.start + tiles / s * c.tile);
+    const double us = std::max(full, c.start + chain / s * c.tile) + (s > 1 ? c.join + (double)s * a.tokens * a.h_kv * a.dh * 16 / 4e6 : 0);
+    if (s == 1 || us < least) {
+      best = s;
+      least = us;
+    }
+  }
+  return best;
 }
 
 // how the work is divided: a function of the sizes alone
@@ -434,9 +439,9 @@ BwdArgs plan_of(const PackedAttn& a) {
   return b;
 }
 // Whether both passes are one launch.  d_head 64: always, they use as many registers.  d_head 128: dQ then runs with one wave per SIMD as
-// dK/dV does, not two (24 / 8 heads, 6600 rows: 297 us apart, 311 together; 18 / 6 heads, 150 rows: 36 and 25)
-bool together(const PackedAttn& a, int units) { return a.dh == 64 || units <= 1024; }
-int64_t marks_bytes(const BwdArgs& b) { return ((int64_t)b.k_units + b.q_units + 63) / 64 * 256; }
+// dK/dV does, not two, which counts where its tiles fill the card many times over (us apart / together: 24 heads on 8, 6600 rows of 24
+// sequences 267 / 250, 15 on 15, 27359 rows of 120 621 / 656, 16 on 2, 8969 rows of 3 630 / 662; 18 on 6, 150 rows 36 / 25).
+bool together(const PackedAttn& a, const BwdArgs& b) { return a.dh == 64 || b.q_units * (rows_met(a) / 64 + 0.5) < 10000; }
 
 template <int DH, int WHAT>
 hipError_t launch_passes(const BwdArgs& b, hipStream_t st) {
@@ -449,16 +454,12 @@ hipError_t launch_passes(const BwdArgs& b, hipStream_t st) {
 
 template <int DH>
 hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
-  const int units = b.k_units + b.q_units;
   hipError_t e;
-  if (together(a, units)) {
+  if (together(a, b)) {
     e = launch_passes<DH, 3>(b, st);
   } else {
     e = launch_passes<DH, 1>(b, st);
     if (e == hipSuccess) e = launch_passes<DH, 2>(b, st);
-    constexpr int lds = 2 * (2 * 64 * DH * 2 + 512);
-    if (e == hipSuccess) e = allow_lds((const void*)packed_bwd_again_kernel<DH>, lds);
-    if (e == hipSuccess) hipLaunchKernelGGL(packed_bwd_again_kernel<DH>, dim3((unsigned)(units < 256 ? units : 256)), dim3(256), lds, st, b);
   }
   if (e != hipSuccess) return e;
   if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
@@ -469,7 +470,7 @@ hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
 
 int64_t packed_bwd_bf16_bytes(const PackedAttn& a) {
   const BwdArgs b = plan_of(a);
-  return marks_bytes(b) + (b.splits > 1 ? (int64_t)b.splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0);
+  return (b.splits > 1 ? (int64_t)b.splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0);
 }
 
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
@@ -482,8 +483,7 @@ hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, cons
   b.dq = (bf16_t*)dq;
   b.dk = (bf16_t*)dk;
   b.dv = (bf16_t*)dv;
-  b.marks = (int32_t*)workspace;
-  b.partial = b.splits > 1 ? (float*)((char*)workspace + marks_bytes(b)) : nullptr;
+  b.partial = b.splits > 1 ? (float*)workspace : nullptr;
   b.scale_log2e = LOG2E_P * o.scale;
   return a.dh == 64 ? run<64>(a, b, st) : run<128>(a, b, st);
 }

@@ -420,7 +420,7 @@ int fwd_form(const PackedAttn& a) {
 }  // namespace
 
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
-  int form = fwd_form(a); // PF_EXP
+  int form = fwd_form(a);
   if (a.dh == 64) {
     switch (form) {
       case 1: return launch_units<64, 1>(a, o, out, lse, st);
