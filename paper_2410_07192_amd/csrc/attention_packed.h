@@ -228,6 +228,13 @@ __device__ __forceinline__ void add_with_care(f32x16* acc, const bf16x8* w, lds_
 // Lets `kernel` have `bytes` of dynamic LDS on the current device
 hipError_t allow_lds(const void* kernel, int bytes);
 
+// Heads of a group that a workgroup of four waves takes: a power of two
+inline int heads_together(const PackedAttn& a) {
+  int heads = 1;
+  while (heads < 4 && (a.h / a.h_kv) % (heads * 2) == 0) heads *= 2;
+  return heads;
+}
+
 // bf16, d_head 64 / 128, all pointers 16-byte aligned, strides in eights
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st);
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,

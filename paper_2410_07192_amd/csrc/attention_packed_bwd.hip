@@ -430,8 +430,7 @@ BwdArgs plan_of(const PackedAttn& a) {
   b.k_blocks = (int32_t)((a.tokens + 127) / 128);
   b.splits = splits_of(a);
   b.k_units = b.k_blocks * a.h_kv * b.splits;
-  b.heads = 1;
-  while (b.heads < 4 && (a.h / a.h_kv) % (b.heads * 2) == 0) b.heads *= 2;
+  b.heads = heads_together(a);
   const int rows = 128 / b.heads;
   b.q_blocks = (int32_t)((a.tokens + rows - 1) / rows);
   b.q_units = b.q_blocks * (a.h / b.heads);

@@ -10,6 +10,7 @@
 // More heads and fewer rows read the same K/V for the same products but end nearer to the causal diagonal and to the ends of sequences.
 #include "attention_packed.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace pf {
@@ -396,12 +397,10 @@ hipError_t launch_units(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* o
 }
 
 template <int DH, int KG>
-hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, int heads, void* out, float* lse, hipStream_t st) {
   constexpr int lds = 2 * KG * 2 * 64 * DH * 2;
   hipError_t e = allow_lds((const void*)packed_fwd_bf16_kernel<DH, KG>, lds);
   if (e != hipSuccess) return e;
-  int heads = 1;
-  while (heads < 4 && (a.h / a.h_kv) % (heads * 2) == 0) heads *= 2;
   const int rows = 128 / heads, log_rows = __builtin_ctz(rows);
   const int64_t blocks = (a.tokens + rows - 1) / rows;
   const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, log_rows, blocks * (a.h / heads) * KG <= 512, LOG2E_P * o.scale};
@@ -409,32 +408,49 @@ hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, fl
   return hipGetLastError();
 }
 
-// 1, 2, 4: independent waves with that many to a unit's keys; 0: shared tiles
-int fwd_form(const PackedAttn& a) {
-  const int64_t units = (a.tokens + 31) / 32 * a.h;
-  if (units <= (a.dh == 64 ? 1024 : 384)) return 4;
-  if (a.dh == 64 && units <= 4096) return 1;
-  return 0;
+// Which form is fastest: shared tiles, a block's keys in one or two parts (8), or independent waves with 1, 2 or 4 to a unit's keys.
+// The estimate of each is the longer of two: its workgroups fill the card's `slots` (start + tiles x full us each), or its longest
+// block's chain counts (start + tiles x alone us); `longest` times the average length is what the longest sequence is taken to be.  The
+// constants are fitted to 260 drawn sizes timed in every form (MI355X): 1.2 % (d_head 64) and 1.7 % (128) off the fastest form on average,
+// 26 % at most.  us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 16.5 / 14.3 / 19.1 / 12.9 / 10.3;
+// 16 sequences up to 2048 72 / 61 / 71 / 83 / 120; 2 up to 8192, 32 on 4 heads 889 / 965 / 1400 / 1490 / 1994; 12 heads of 64, 32 up to 512
+// 26.8 / 33.6 / 26.5 / 28.0 / 33.6; 6 heads of 64, 1942 rows 44.7 / 31.8 / 43.0 / 25.4 / 17.0.
+enum FwdForm { SHARED_1, SHARED_2, WAVES_1, WAVES_2, WAVES_4 };
+FwdForm fwd_form(const PackedAttn& a, int heads) {
+  struct Cost { FwdForm form; int parts; double start, alone, full; };
+  static const Cost costs64[] = {{SHARED_1, 1, 5.03, 0.99, 1.2}, {WAVES_1, 1, 2.31, 1.48, 1.7}, {WAVES_2, 2, 5.42, 1.53, 0.66}, {WAVES_4, 4, 3.78, 0.79, 2.68}};
+  static const Cost costs128[] = {{SHARED_1, 1, 4.28, 1.72, 1.27}, {SHARED_2, 2, 4.71, 1.55, 2.23}, {WAVES_1, 1, 3.0, 1.25, 1.42}, {WAVES_2, 2, 3.71, 1.05, 2.01},
+                                  {WAVES_4, 4, 4.32, 1.09, 1.05}};
+  const bool small = a.dh == 64;
+  const double length = (double)a.tokens / (a.n_seq > 1 ? a.n_seq : 1), met = a.causal ? length / 2 : length;
+  const double longest = a.n_seq > 1 ? std::min((double)a.tokens, (small ? 1.79 : 1.99) * length) : length;
+  FwdForm best = SHARED_1;
+  double least = 0;
+  for (const Cost* c = small ? costs64 : costs128; c != (small ? costs64 + 4 : costs128 + 5); ++c) {
+    const bool shared = c->form == SHARED_1 || c->form == SHARED_2;
+    const double rows = shared ? 128.0 / heads : 32.0;
+    const double blocks = ceil((double)a.tokens / rows) * a.h;
+    const double full_card = shared ? blocks / heads * c->parts / 512 : blocks * c->parts / 4 / (small ? 512 : 256);
+    const double tiles = ((met + rows) / 64 + 0.5) / c->parts, chain = ((longest + rows) / 64 + 0.5) / c->parts;
+    const double us = std::max(std::max(1.0, full_card) * (c->start + (shared ? tiles : ceil(tiles)) * c->full), c->start + (shared ? chain : ceil(chain)) * c->alone);
+    if (c->form == SHARED_1 || us < least) {
+      best = c->form;
+      least = us;
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
-  int form = fwd_form(a);
-  if (a.dh == 64) {
-    switch (form) {
-      case 1: return launch_units<64, 1>(a, o, out, lse, st);
-      case 2: return launch_units<64, 2>(a, o, out, lse, st);
-      case 4: return launch_units<64, 4>(a, o, out, lse, st);
-      default: return launch<64, 1>(a, o, out, lse, st);
-    }
-  }
-  switch (form) {
-    case 1: return launch_units<128, 1>(a, o, out, lse, st);
-    case 2: return launch_units<128, 2>(a, o, out, lse, st);
-    case 4: return launch_units<128, 4>(a, o, out, lse, st);
-    case 8: return launch<128, 2>(a, o, out, lse, st);
-    default: return launch<128, 1>(a, o, out, lse, st);
+  const int heads = heads_together(a);
+  switch (fwd_form(a, heads)) {
+    case WAVES_1: return a.dh == 64 ? launch_units<64, 1>(a, o, out, lse, st) : launch_units<128, 1>(a, o, out, lse, st);
+    case WAVES_2: return a.dh == 64 ? launch_units<64, 2>(a, o, out, lse, st) : launch_units<128, 2>(a, o, out, lse, st);
+    case WAVES_4: return a.dh == 64 ? launch_units<64, 4>(a, o, out, lse, st) : launch_units<128, 4>(a, o, out, lse, st);
+    case SHARED_2: return launch<128, 2>(a, o, heads, out, lse, st);   // (d_head 64 never)
+    default: return a.dh == 64 ? launch<64, 1>(a, o, heads, out, lse, st) : launch<128, 1>(a, o, heads, out, lse, st);
   }
 }
 
