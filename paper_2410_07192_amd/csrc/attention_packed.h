@@ -240,5 +240,8 @@ hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
                            void* dv, void* workspace, hipStream_t st);
 int64_t packed_bwd_bf16_bytes(const PackedAttn& a);   // of workspace
+// fp32 sums of dK and dV of several splits, [split][dK, dV][tokens][K/V heads * d_head]: their size, and what makes dk and dv of them
+int64_t packed_partial_bytes(const PackedAttn& a, int splits);
+hipError_t packed_join(const PackedAttn& a, const float* partial, int splits, void* dk, void* dv, hipStream_t st);
 
 }  // namespace pf

@@ -196,28 +196,6 @@ __global__ __launch_bounds__(256) void packed_fwd_f32_kernel(PackedQkv<T> a, T* 
   }
 }
 
-// dsum[head][row] = dO . O: eight columns a lane, a row's lanes next to each other
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void packed_bwd_prep_kernel(const T* __restrict__ out, const T* __restrict__ dout, float* __restrict__ dsum,
-                                                              int64_t ld, int32_t tokens, int32_t h, int32_t dh) {
-  const int per = dh / 8;   // lanes of a head: 1, 2, 4, 8 or 16
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)tokens * h * per;
-  const int64_t at = i < n ? i : n - 1;   // lanes past the end repeat the last one
-  const int64_t row = at / (h * per);
-  const int hd = (int)(at / per % h), c = (int)(at % per) * 8;
-  const T* po = out + row * ld + hd * dh + c;
-  const T* pd = dout + row * ld + hd * dh + c;
-  float s = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; j += 4) {
-    const f32x4 x = row4<VEC>(po + j), y = row4<VEC>(pd + j);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s = fmaf(x[e], y[e], s);
-  }
-  for (int o = per / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (i < n && c == 0) dsum[(int64_t)hd * tokens + row] = s;
-}
-
 // the waves' sums of one 32 x DH block, in LDS, to global memory: the rows in `live`
 template <int DH, bool VEC, typename T>
 __device__ __forceinline__ void join_rows(const float (*sO)[32][(DH + 31) / 32 * 32 + 4], uint64_t live, T* dst, int64_t ld, float scale) {
@@ -241,20 +219,33 @@ __device__ __forceinline__ void put_acc(float (*s)[DT * 32 + 4], const f32x16* a
       *(f32x4*)&s[lr][dt * 32 + rg * 8 + g * 4] = f32x4{acc[dt][rg * 4], acc[dt][rg * 4 + 1], acc[dt][rg * 4 + 2], acc[dt][rg * 4 + 3]};
 }
 
-// dK, dV: 32 keys of one K/V head; the waves share the tiles of 32 queries of all heads of its group
+template <typename T>
+struct BwdF32 {
+  PackedQkv<T> o;
+  const T *out, *dout;
+  const float* lse;
+  T *dq, *dk, *dv;
+  float* partial;          // [split][dK, dV][tokens][K/V heads * d_head], or null with one split
+  int32_t splits, k_units;
+};
+
+// dK, dV: 32 keys of one K/V head; the waves share the tiles of 32 queries of all heads of its group, or of a split of them
 template <typename T, int DH, bool VEC>
-__global__ __launch_bounds__(256, 1) void packed_bwd_dkv_f32_kernel(PackedQkv<T> a, const T* __restrict__ dout, const float* __restrict__ lse,
-                                                                    const float* __restrict__ dsum, T* __restrict__ dk, T* __restrict__ dv) {
-  constexpr int KK = DH / 8, DT = (DH + 31) / 32, LD = DT * 32 + 4;
-  __shared__ __align__(16) float sO[NW][32][LD];
+__device__ __forceinline__ void dkv_f32_block(const BwdF32<T>& b, int unit, float (*sO)[32][(DH + 31) / 32 * 32 + 4]) {
+  constexpr int KK = DH / 8, DT = (DH + 31) / 32;
+  const PackedQkv<T>& a = b.o;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 31, g = lane >> 5;
   const int n_kv = a.h / a.group, T_ = a.rows.tokens;
-  const int hk = (int)(blockIdx.x % (uint32_t)n_kv), k_blk = (int)(blockIdx.x / (uint32_t)n_kv) * 32;   // causal: the long ones first
+  const uint32_t per = (uint32_t)(n_kv * b.splits);
+  const int hk = (int)((uint32_t)unit % per) % n_kv, split = (int)((uint32_t)unit % per) / n_kv, k_blk = (int)((uint32_t)unit / per) * 32;
   const int key = k_blk + lr;
-  f32x4 fk[KK], fv[KK];
-  {
-    const T* pk = a.k + (int64_t)min(key, T_ - 1) * a.ld_k + hk * DH + g * 4;
-    const T* pv = a.v + (int64_t)min(key, T_ - 1) * a.ld_v + hk * DH + g * 4;
+  // the block's own rows: d_head 128 has no registers for them beside 128 of sums (239 were spilled) and reads them with every tile, from L1
+  constexpr bool KEEP = DH < 128;
+  constexpr int UNROLL = KEEP ? KK : 4;
+  f32x4 fk[KEEP ? KK : 1], fv[KEEP ? KK : 1];
+  const T* pk = a.k + (int64_t)min(key, T_ - 1) * a.ld_k + hk * DH + g * 4;
+  const T* pv = a.v + (int64_t)min(key, T_ - 1) * a.ld_v + hk * DH + g * 4;
+  if constexpr (KEEP) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       fk[kk] = row4<VEC>(pk + kk * 8) * a.scale;
@@ -270,34 +261,48 @@ __global__ __launch_bounds__(256, 1) void packed_bwd_dkv_f32_kernel(PackedQkv<T>
 #pragma unroll
     for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
   const int tiles = (q_end - q_begin + 31) / 32;
-  for (int64_t it = wave; it < (int64_t)tiles * a.group; it += NW) {
+  const int64_t all = (int64_t)(tiles > 0 ? tiles : 0) * a.group, end = all * (split + 1) / b.splits;
+  for (int64_t it = all * split / b.splits + wave; it < end; it += NW) {
     const int hd = hk * a.group + (int)(it / tiles), q0 = q_begin + (int)(it % tiles) * 32;
     const T* qh = a.q + hd * DH;
-    const T* dh_ = dout + hd * DH;
+    const T* dh_ = b.dout + hd * DH;
     const int q_row = min(q0 + lr, q_end - 1);
     const T* pq = qh + (int64_t)q_row * a.ld_q + g * 4;
     const T* pd = dh_ + (int64_t)q_row * a.ld_out + g * 4;
+    const T* po = b.out + hd * DH + (int64_t)q_row * a.ld_out + g * 4;
+    float D = 0.f;   // of row q_row
     f32x16 s, dp;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
+    if constexpr (!KEEP) asm volatile("" : "+v"(pk), "+v"(pv));   // or the compiler reads them once after all
+#pragma unroll UNROLL
     for (int kk = 0; kk < KK; ++kk) {
-      const f32x4 x = row4<VEC>(pq + kk * 8), y = row4<VEC>(pd + kk * 8);
+      const f32x4 x = row4<VEC>(pq + kk * 8), y = row4<VEC>(pd + kk * 8), o = row4<VEC>(po + kk * 8);
+      f32x4 xk, xv;
+      if constexpr (KEEP) {
+        xk = fk[kk];
+        xv = fv[kk];
+      } else {
+        xk = row4<VEC>(pk + kk * 8) * a.scale;
+        xv = row4<VEC>(pv + kk * 8);
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], fk[kk][j], s, 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x2f32(y[j], fv[kk][j], dp, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], xk[j], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x2f32(y[j], xv[j], dp, 0, 0, 0);
+        D = fmaf(y[j], o[j], D);
       }
     }
+    D += __shfl_xor(D, 32, 64);
     const bool masked = q0 < in_lo || q0 + 31 >= in_hi;
-    const float* L = lse + (int64_t)hd * T_;
-    const float* D = dsum + (int64_t)hd * T_;
+    const float L = b.lse[(int64_t)hd * T_ + q_row];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int q = q0 + reg_row(r, g), qc = min(q, q_end - 1);
+      const int q = q0 + reg_row(r, g);   // L and D of row q are in lane q - q0
       const bool hidden = masked && (q < own.lo || q >= own.hi);
-      const float p = hidden ? 0.f : __expf(s[r] - L[qc]);
-      dp[r] = hidden ? 0.f : p * (dp[r] - D[qc]);
+      const float Lq = __shfl(L, reg_row(r, g), 64), Dq = __shfl(D, reg_row(r, g), 64);
+      const float p = hidden ? 0.f : __expf(s[r] - Lq);
+      dp[r] = hidden ? 0.f : p * (dp[r] - Dq);
       s[r] = p;
     }
     auto seen = [&](int i) { return q0 + i >= own.lo && q0 + i < own.hi; };
@@ -316,36 +321,44 @@ __global__ __launch_bounds__(256, 1) void packed_bwd_dkv_f32_kernel(PackedQkv<T>
   const uint64_t live = __ballot(own.lo < own.hi);
   put_acc<DT>(sO[wave], accK);
   __syncthreads();
-  join_rows<DH, VEC>(sO, live, dk + (int64_t)k_blk * a.ld_k + hk * DH, a.ld_k, a.scale);
+  const int64_t at = (int64_t)split * 2 * T_ + k_blk, ld = n_kv * DH;
+  if (b.partial) join_rows<DH, true>(sO, live, b.partial + at * ld + hk * DH, ld, 1.0f);
+  else join_rows<DH, VEC>(sO, live, b.dk + (int64_t)k_blk * a.ld_k + hk * DH, a.ld_k, a.scale);
   __syncthreads();
   put_acc<DT>(sO[wave], accV);
   __syncthreads();
-  join_rows<DH, VEC>(sO, live, dv + (int64_t)k_blk * a.ld_v + hk * DH, a.ld_v, 1.0f);
+  if (b.partial) join_rows<DH, true>(sO, live, b.partial + (at + T_) * ld + hk * DH, ld, 1.0f);
+  else join_rows<DH, VEC>(sO, live, b.dv + (int64_t)k_blk * a.ld_v + hk * DH, a.ld_v, 1.0f);
 }
 
 // dQ: 32 queries of one head; the waves share the tiles of 32 keys
 template <typename T, int DH, bool VEC>
-__global__ __launch_bounds__(256, 1) void packed_bwd_dq_f32_kernel(PackedQkv<T> a, const T* __restrict__ dout, const float* __restrict__ lse,
-                                                                   const float* __restrict__ dsum, T* __restrict__ dq) {
-  constexpr int KK = DH / 8, DT = (DH + 31) / 32, LD = DT * 32 + 4;
-  __shared__ __align__(16) float sO[NW][32][LD];
+__device__ __forceinline__ void dq_f32_block(const BwdF32<T>& b, int unit, float (*sO)[32][(DH + 31) / 32 * 32 + 4]) {
+  constexpr int KK = DH / 8, DT = (DH + 31) / 32;
+  const PackedQkv<T>& a = b.o;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 31, g = lane >> 5;
-  const int hd = (int)(blockIdx.x % (uint32_t)a.h), T_ = a.rows.tokens;
-  const int q_blk = ((T_ + 31) / 32 - 1 - (int)(blockIdx.x / (uint32_t)a.h)) * 32;
+  const int hd = (int)((uint32_t)unit % (uint32_t)a.h), T_ = a.rows.tokens;
+  const int q_blk = ((T_ + 31) / 32 - 1 - (int)((uint32_t)unit / (uint32_t)a.h)) * 32;
   const int q_row = q_blk + lr, qc = min(q_row, T_ - 1);
   const T* kh = a.k + hd / a.group * DH;
   const T* vh = a.v + hd / a.group * DH;
   f32x4 fq[KK], fd[KK];
+  float D = 0.f;
   {
     const T* pq = a.q + (int64_t)qc * a.ld_q + hd * DH + g * 4;
-    const T* pd = dout + (int64_t)qc * a.ld_out + hd * DH + g * 4;
+    const T* pd = b.dout + (int64_t)qc * a.ld_out + hd * DH + g * 4;
+    const T* po = b.out + (int64_t)qc * a.ld_out + hd * DH + g * 4;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       fq[kk] = row4<VEC>(pq + kk * 8) * a.scale;
       fd[kk] = row4<VEC>(pd + kk * 8);
+      const f32x4 o = row4<VEC>(po + kk * 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) D = fmaf(fd[kk][j], o[j], D);
     }
   }
-  const float L = lse[(int64_t)hd * T_ + qc], D = dsum[(int64_t)hd * T_ + qc];
+  D += __shfl_xor(D, 32, 64);
+  const float L = b.lse[(int64_t)hd * T_ + qc];
   const Span own = keys_of(a.rows, q_blk, q_row, a.causal);
   const int k_begin = lane_value(own.lo, 0), k_end = lane_value(own.hi, 31);
   const int in_lo = lane_value(own.lo, 31), in_hi = lane_value(own.hi, 0);
@@ -387,7 +400,53 @@ __global__ __launch_bounds__(256, 1) void packed_bwd_dq_f32_kernel(PackedQkv<T> 
   put_acc<DT>(sO[wave], acc);
   const uint64_t live = __ballot(own.lo < own.hi);
   __syncthreads();
-  join_rows<DH, VEC>(sO, live, dq + (int64_t)q_blk * a.ld_q + hd * DH, a.ld_q, a.scale);
+  join_rows<DH, VEC>(sO, live, b.dq + (int64_t)q_blk * a.ld_q + hd * DH, a.ld_q, a.scale);
+}
+
+// Both passes: the dK/dV workgroups first, they are the longer ones
+template <typename T, int DH, bool VEC>
+__global__ __launch_bounds__(256, 1) void packed_bwd_f32_kernel(BwdF32<T> b) {
+  __shared__ __align__(16) float sO[NW][32][(DH + 31) / 32 * 32 + 4];
+  const int unit = (int)blockIdx.x;
+  if (unit < b.k_units) dkv_f32_block<T, DH, VEC>(b, unit, sO);
+  else dq_f32_block<T, DH, VEC>(b, unit - b.k_units, sO);
+}
+
+// dK, dV from the splits' sums [split][dK, dV][tokens][width]: four columns a thread, rows that are in a sequence
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void packed_bwd_join_kernel(const float* __restrict__ partial, PackedRows rows, int32_t width, int32_t splits, T* __restrict__ dk,
+                                                              T* __restrict__ dv, int64_t ld_k, int64_t ld_v, float scale) {
+  const int T_ = rows.tokens, per = width / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int row = (int)(i / per), c = (int)(i % per) * 4;
+  const int first = rows.start ? rows.start[0] : 0, last = rows.start ? rows.start[rows.n_seq] : T_;
+  if (i >= (int64_t)T_ * per || row < first || row >= last) return;
+  const bool is_v = blockIdx.y != 0;
+  const float* p = partial + ((int64_t)(is_v ? T_ : 0) + row) * width + c;
+  f32x4 x = *(const f32x4*)p;
+  for (int s = 1; s < splits; ++s) x += *(const f32x4*)(p + (int64_t)s * 2 * T_ * width);
+  if (!is_v) x *= scale;
+  const float r4[4] = {x[0], x[1], x[2], x[3]};
+  put4<VEC>(is_v ? dv + (int64_t)row * ld_v + c : dk + (int64_t)row * ld_k + c, r4);
+}
+
+// dsum[head][row] = dO . O: eight columns a lane, a row's lanes next to each other
+__global__ __launch_bounds__(256) void packed_bwd_prep_kernel(const bf16_t* __restrict__ out, const bf16_t* __restrict__ dout, float* __restrict__ dsum,
+                                                              int64_t ld, int32_t tokens, int32_t h, int32_t dh) {
+  const int per = dh / 8;   // lanes of a head: 8 or 16
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)tokens * h * per;
+  const int64_t at = i < n ? i : n - 1;   // lanes past the end repeat the last one
+  const int64_t row = at / (h * per);
+  const int hd = (int)(at / per % h), c = (int)(at % per) * 8;
+  const bf16_t* po = out + row * ld + hd * dh + c;
+  const bf16_t* pd = dout + row * ld + hd * dh + c;
+  float x[8], y[8], s = 0.f;
+  load8(po, x);
+  load8(pd, y);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s = fmaf(x[j], y[j], s);
+  for (int o = per / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (i < n && c == 0) dsum[(int64_t)hd * tokens + row] = s;
 }
 
 template <typename T>
@@ -405,20 +464,39 @@ bool aligned16(const PackedAttn& a, std::initializer_list<const void*> ptrs) {
 // whether bf16 products are used: they round P and dS, as the storage type rounds the results, and are 16 times as fast
 bool by_bf16(const PackedAttn& a) { return a.dtype == PF_DTYPE_BF16_ && (a.dh == 64 || a.dh == 128); }
 
+template <typename T, bool VEC>
+hipError_t join(const PackedAttn& a, const float* partial, int splits, void* dk, void* dv, hipStream_t st) {
+  const int width = a.h_kv * a.dh;
+  hipLaunchKernelGGL((packed_bwd_join_kernel<T, VEC>), dim3((unsigned)((a.tokens * (width / 4) + 255) / 256), 2), dim3(256), 0, st, partial,
+                     PackedRows{a.seq_start, a.n_seq, (int32_t)a.tokens}, width, splits, (T*)dk, (T*)dv, a.ld_k, a.ld_v, 1.0f / sqrtf((float)a.dh));
+  return hipGetLastError();
+}
+
 template <typename T, int DH, bool VEC>
 hipError_t fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse, hipStream_t st) {
   const unsigned grid = (unsigned)((a.tokens + 31) / 32 * a.h);
   hipLaunchKernelGGL((packed_fwd_f32_kernel<T, DH, VEC>), dim3(grid), dim3(256), 0, st, operands<T>(a, q, k, v), (T*)out, lse);
   return hipGetLastError();
 }
+// Splits of a block's tiles in dK/dV: as many as fill the card, four tiles (one a wave) to each or more if sequences were all as long as
+// they are on average.  (4 heads on 2 of 64, 262 fp32 rows of 4 sequences: 18 blocks of 10 tiles; 36 us with one split and a launch for each pass, 20 with 3 and one launch; 16 of 64 and 4096 rows: 914, 841.)
+int splits_f32(const PackedAttn& a) {
+  const int64_t units = (a.tokens + 31) / 32 * a.h_kv, length = a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
+  const int64_t tiles = ((a.causal ? length / 2 : length) + 63) / 32 * (a.h / a.h_kv);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(256 + units - 1) / units, (tiles + 3) / 4, 8}));
+}
+
 template <typename T, int DH, bool VEC>
-hipError_t bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* dout, const float* lse, const float* dsum,
-               void* dq, void* dk, void* dv, hipStream_t st) {
-  const PackedQkv<T> o = operands<T>(a, q, k, v);
+hipError_t bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* out, const void* dout, const float* lse, void* dq,
+               void* dk, void* dv, float* partial, hipStream_t st) {
+  BwdF32<T> b{operands<T>(a, q, k, v), (const T*)out, (const T*)dout, lse, (T*)dq, (T*)dk, (T*)dv, nullptr, splits_f32(a), 0};
+  if (b.splits > 1) b.partial = partial;
   const int64_t blocks = (a.tokens + 31) / 32;
-  hipLaunchKernelGGL((packed_bwd_dkv_f32_kernel<T, DH, VEC>), dim3((unsigned)(blocks * a.h_kv)), dim3(256), 0, st, o, (const T*)dout, lse, dsum, (T*)dk, (T*)dv);
-  hipLaunchKernelGGL((packed_bwd_dq_f32_kernel<T, DH, VEC>), dim3((unsigned)(blocks * a.h)), dim3(256), 0, st, o, (const T*)dout, lse, dsum, (T*)dq);
-  return hipGetLastError();
+  b.k_units = (int32_t)(blocks * a.h_kv * b.splits);
+  hipLaunchKernelGGL((packed_bwd_f32_kernel<T, DH, VEC>), dim3((unsigned)(b.k_units + blocks * a.h)), dim3(256), 0, st, b);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || b.splits == 1) return e;
+  return VEC ? packed_join(a, partial, b.splits, dk, dv, st) : join<T, VEC>(a, partial, b.splits, dk, dv, st);
 }
 
 #define PF_BY_SHAPE(CALL)                                                                        \
@@ -449,31 +527,33 @@ hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* 
 #undef PF_FWD
 }
 
+int64_t packed_partial_bytes(const PackedAttn& a, int splits) { return splits > 1 ? (int64_t)splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0; }
+
+hipError_t packed_join(const PackedAttn& a, const float* partial, int splits, void* dk, void* dv, hipStream_t st) {
+  return a.dtype == PF_DTYPE_F32_ ? join<float, true>(a, partial, splits, dk, dv, st) : join<bf16_t, true>(a, partial, splits, dk, dv, st);
+}
+
 static int64_t dsum_bytes(const PackedAttn& a) { return ((int64_t)a.h * a.tokens * 4 + 255) / 256 * 256; }
-int64_t attention_packed_bwd_bytes(const PackedAttn& a) { return dsum_bytes(a) + (by_bf16(a) ? packed_bwd_bf16_bytes(a) : 0); }
+
+// enough for either kernel: which one runs depends on the alignment of the call's pointers too
+int64_t attention_packed_bwd_bytes(const PackedAttn& a) {
+  const int64_t f32 = packed_partial_bytes(a, splits_f32(a));
+  return std::max<int64_t>(256, by_bf16(a) ? std::max(f32, dsum_bytes(a) + packed_bwd_bf16_bytes(a)) : f32);
+}
 
 hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* out, const void* dout,
                                 const float* lse, void* dq, void* dk, void* dv, void* workspace, hipStream_t st) {
   const bool vec = aligned16(a, {q, k, v, out, dout, dq, dk, dv});
-  float* dsum = (float*)workspace;
-  const int64_t n = a.tokens * a.h * (a.dh / 8);
-  const dim3 grid((unsigned)((n + 255) / 256)), block(256);
-#define PF_PREP(T, V)                                                                                                                  \
-  hipLaunchKernelGGL((packed_bwd_prep_kernel<T, V>), grid, block, 0, st, (const T*)out, (const T*)dout, dsum, a.ld_out, (int32_t)a.tokens, \
-                     a.h, a.dh)
-  if (a.dtype == PF_DTYPE_F32_) {
-    if (vec) PF_PREP(float, true);
-    else PF_PREP(float, false);
-  } else {
-    if (vec) PF_PREP(bf16_t, true);
-    else PF_PREP(bf16_t, false);
-  }
-#undef PF_PREP
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (vec && by_bf16(a))
+  if (vec && by_bf16(a)) {
+    float* dsum = (float*)workspace;
+    const int64_t n = a.tokens * a.h * (a.dh / 8);
+    hipLaunchKernelGGL(packed_bwd_prep_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const bf16_t*)out, (const bf16_t*)dout, dsum, a.ld_out,
+                       (int32_t)a.tokens, a.h, a.dh);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     return packed_bwd_bf16(a, operands<bf16_t>(a, q, k, v), dout, lse, dsum, dq, dk, dv, (char*)workspace + dsum_bytes(a), st);
-#define PF_BWD(T, D, V) bwd<T, D, V>(a, q, k, v, dout, lse, dsum, dq, dk, dv, st)
+  }
+#define PF_BWD(T, D, V) bwd<T, D, V>(a, q, k, v, out, dout, lse, dq, dk, dv, (float*)workspace, st)
   PF_BY_SHAPE(PF_BWD);
 #undef PF_BWD
 }

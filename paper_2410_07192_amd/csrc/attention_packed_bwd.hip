@@ -239,33 +239,6 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   return odd;
 }
 
-// dK, dV from the splits' sums: eight columns a thread, rows that are in a sequence
-template <int DH>
-__global__ __launch_bounds__(256) void packed_bwd_join_kernel(BwdArgs a) {
-  const int n_kv = a.o.h / a.o.group, T = a.o.rows.tokens, per = n_kv * DH / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int row = (int)(i / per), c = (int)(i % per) * 8;
-  const int first = a.o.rows.start ? a.o.rows.start[0] : 0, last = a.o.rows.start ? a.o.rows.start[a.o.rows.n_seq] : T;
-  if (i >= (int64_t)T * per || row < first || row >= last) return;
-  const bool is_v = blockIdx.y != 0;
-  const float* p = a.partial + ((int64_t)(is_v ? T : 0) + row) * (n_kv * DH) + c;
-  float x[8];
-  load8(p, x);
-  for (int s = 1; s < a.splits; ++s) {
-    float y[8];
-    load8(p + (int64_t)s * 2 * T * (n_kv * DH), y);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] += y[j];
-  }
-  if (!is_v) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= a.o.scale;
-    store8(a.dk + (int64_t)row * a.o.ld_k + c, x);
-  } else {
-    store8(a.dv + (int64_t)row * a.o.ld_v + c, x);
-  }
-}
-
 // ---- dQ ----------------------------------------------------------------------------------------------------------------------
 template <int DH, bool CAREFUL>
 __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem, int* s_span) {
@@ -461,16 +434,12 @@ hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
     if (e == hipSuccess) e = launch_passes<DH, 2>(b, st);
   }
   if (e != hipSuccess) return e;
-  if (b.splits > 1) hipLaunchKernelGGL(packed_bwd_join_kernel<DH>, dim3((unsigned)((a.tokens * a.h_kv * (DH / 8) + 255) / 256), 2), dim3(256), 0, st, b);
-  return hipGetLastError();
+  return b.splits > 1 ? packed_join(a, b.partial, b.splits, b.dk, b.dv, st) : hipSuccess;
 }
 
 }  // namespace
 
-int64_t packed_bwd_bf16_bytes(const PackedAttn& a) {
-  const BwdArgs b = plan_of(a);
-  return (b.splits > 1 ? (int64_t)b.splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0);
-}
+int64_t packed_bwd_bf16_bytes(const PackedAttn& a) { return packed_partial_bytes(a, splits_of(a)); }
 
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,
                            void* dv, void* workspace, hipStream_t st) {
