@@ -58,8 +58,8 @@ struct FwdRows {
         s[ks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fk), fq[kk], s[ks], 0, 0, 0);
       }
   }
-  __device__ __forceinline__ float exponentials(f32x16* s) const {   // their sum
-    const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
+  __device__ __forceinline__ float exponentials(f32x16* s, bool none = false) const {   // their sum; none: of keys that the row does not see
+    const float neg_m = none ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -72,14 +72,19 @@ struct FwdRows {
   }
   // Scores of the tile at key k0 into probabilities.  masked: not every row sees every key; fresh: nothing has been added yet.
   __device__ __forceinline__ void probabilities(const char* sK, f32x16* s, int k0, bool masked, bool fresh) {
-    if (!(masked || fresh)) {
-      const float tot = exponentials(s);
+    // Most tiles that are masked lie in the block's first sequence and none of its rows of the next one sees them: a lane's row sees all of
+    // the tile or nothing of it, and has its reference point or needs none (2048 rows behind 5 others, 16 heads on 2 of 128:
+    // 65 us with every such tile masked by element, 52 so).
+    const bool all = own.lo <= k0 && own.hi >= k0 + 64, none = own.hi <= k0 || own.lo >= k0 + 64;
+    if (!fresh && !(masked && __any(!(none || (all && m_ref != -INFINITY))))) {
+      const float tot = exponentials(s, none);
       if (!__any(!(tot <= 128.0f))) {   // (also infinite or NaN)
         l_run += tot;
         return;
       }
       scores(sK, s);
-    } else if (masked) {
+    }
+    if (masked) {
       const int lo = own.lo - k0 - 4 * g, hi = own.hi - k0 - 4 * g;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
@@ -162,8 +167,9 @@ struct FwdGrid {
 };
 // A workgroup's block of rows and heads: four waves share K/V tiles.  KG = 2: twice four, the second four with every other tile, so
 // that a block's own chain over the keys is half as long; their sums meet in LDS.
+// Registers for three waves a SIMD (d_head 64; 12 sequences of 1024, 16 heads on 4: 46.6 us, 53.0 with two; four do not fit, 108) or two.
 template <int DH, int KG>
-__global__ __launch_bounds__(256 * KG, 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
+__global__ __launch_bounds__(256 * KG, DH == 64 ? 3 : 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
   constexpr int NW = 4, TILE = 64 * DH * 2, BUF = KG * 2 * TILE, DT = DH / 32, LD = DH + 4;
   static_assert(KG == 1 || NW * 32 * LD * 4 <= 2 * BUF, "O of one part fits the buffers");
   extern __shared__ __align__(16) char smem[];   // two buffers of KG (K tile | V tile)
@@ -403,36 +409,39 @@ hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, int heads, vo
   if (e != hipSuccess) return e;
   const int rows = 128 / heads, log_rows = __builtin_ctz(rows);
   const int64_t blocks = (a.tokens + rows - 1) / rows;
-  const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, log_rows, blocks * (a.h / heads) * KG <= 512, LOG2E_P * o.scale};
+  const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, log_rows, blocks * (a.h / heads) * KG <= (DH == 64 ? 768 : 512), LOG2E_P * o.scale};
   hipLaunchKernelGGL((packed_fwd_bf16_kernel<DH, KG>), dim3((unsigned)(blocks * grid.groups)), dim3(256 * KG), lds, st, o, (bf16_t*)out, lse, grid);
   return hipGetLastError();
 }
 
-// Which form is fastest: shared tiles, a block's keys in one or two parts (8), or independent waves with 1, 2 or 4 to a unit's keys.
-// The estimate of each is the longer of two: its workgroups fill the card's `slots` (start + tiles x full us each), or its longest
-// block's chain counts (start + tiles x alone us); `longest` times the average length is what the longest sequence is taken to be.  The
-// constants are fitted to 260 drawn sizes timed in every form (MI355X): 1.2 % (d_head 64) and 1.7 % (128) off the fastest form on average,
-// 26 % at most.  us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 16.5 / 14.3 / 19.1 / 12.9 / 10.3;
-// 16 sequences up to 2048 72 / 61 / 71 / 83 / 120; 2 up to 8192, 32 on 4 heads 889 / 965 / 1400 / 1490 / 1994; 12 heads of 64, 32 up to 512
-// 26.8 / 33.6 / 26.5 / 28.0 / 33.6; 6 heads of 64, 1942 rows 44.7 / 31.8 / 43.0 / 25.4 / 17.0.
+// Which form is fastest: shared tiles, a block's keys in one or two parts, or independent waves with 1, 2 or 4 to a unit's keys.  The
+// estimate of each is the longer of two times and some of the other: its workgroups go through the card (start + tiles x full us, times
+// the number of fillings of its `slots`), and its longest block's chain (start + tiles x alone us).  Lengths are on the device, so the
+// longest sequence is taken to be twice the average.  The constants are fitted to 600 sizes timed in every form (MI355X): 2.0 % (d_head 64)
+// and 1.6 % (128) off the fastest form on average, 47 % at most; the best single form would be 16 % and 26 % off.
+// us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 14.9 / 13.9 / 15.8 / 12.1 / 10.0; 16 sequences up
+// to 2048 59 / 58 / 65 / 83 / 119; 2 up to 8192, 32 on 4 heads 868 / 977 / 1325 / 1415 / 1816; 12 heads of 64, 32 up to 512
+// 23.5 / - / 24.6 / 27.6 / 34.4.
 enum FwdForm { SHARED_1, SHARED_2, WAVES_1, WAVES_2, WAVES_4 };
 FwdForm fwd_form(const PackedAttn& a, int heads) {
-  struct Cost { FwdForm form; int parts; double start, alone, full; };
-  static const Cost costs64[] = {{SHARED_1, 1, 5.03, 0.99, 1.2}, {WAVES_1, 1, 2.31, 1.48, 1.7}, {WAVES_2, 2, 5.42, 1.53, 0.66}, {WAVES_4, 4, 3.78, 0.79, 2.68}};
-  static const Cost costs128[] = {{SHARED_1, 1, 4.28, 1.72, 1.27}, {SHARED_2, 2, 4.71, 1.55, 2.23}, {WAVES_1, 1, 3.0, 1.25, 1.42}, {WAVES_2, 2, 3.71, 1.05, 2.01},
-                                  {WAVES_4, 4, 4.32, 1.09, 1.05}};
-  const bool small = a.dh == 64;
-  const double length = (double)a.tokens / (a.n_seq > 1 ? a.n_seq : 1), met = a.causal ? length / 2 : length;
-  const double longest = a.n_seq > 1 ? std::min((double)a.tokens, (small ? 1.79 : 1.99) * length) : length;
+  struct Cost { FwdForm form; int parts, slots; double start, full, alone; };
+  static const Cost costs64[] = {{SHARED_1, 1, 768, 5.85, 2.14, 0.91}, {WAVES_1, 1, 512, 5.66, 1.61, 0.85}, {WAVES_2, 2, 512, 6.01, 1.43, 0.79},
+                                 {WAVES_4, 4, 512, 5.49, 1.36, 0.82}};
+  static const Cost costs128[] = {{SHARED_1, 1, 512, 7.24, 2.30, 1.25}, {SHARED_2, 2, 512, 8.49, 2.38, 1.63}, {WAVES_1, 1, 256, 6.96, 1.70, 1.32},
+                                  {WAVES_2, 2, 256, 7.44, 1.63, 1.11}, {WAVES_4, 4, 256, 6.51, 1.72, 0.99}};
+  const bool small = a.dh == 64, several = a.n_seq > 1;
+  const double length = (double)a.tokens / (several ? a.n_seq : 1);
+  const double longest = several ? std::min((double)a.tokens, 2 * length) : length, met = (several ? 1.5 : 1.0) * length / (a.causal ? 2 : 1);
   FwdForm best = SHARED_1;
   double least = 0;
   for (const Cost* c = small ? costs64 : costs128; c != (small ? costs64 + 4 : costs128 + 5); ++c) {
     const bool shared = c->form == SHARED_1 || c->form == SHARED_2;
     const double rows = shared ? 128.0 / heads : 32.0;
-    const double blocks = ceil((double)a.tokens / rows) * a.h;
-    const double full_card = shared ? blocks / heads * c->parts / 512 : blocks * c->parts / 4 / (small ? 512 : 256);
+    const double workgroups = ceil(a.tokens / rows) * a.h * c->parts / (shared ? heads : 4);
     const double tiles = ((met + rows) / 64 + 0.5) / c->parts, chain = ((longest + rows) / 64 + 0.5) / c->parts;
-    const double us = std::max(std::max(1.0, full_card) * (c->start + (shared ? tiles : ceil(tiles)) * c->full), c->start + (shared ? chain : ceil(chain)) * c->alone);
+    const double all = workgroups / c->slots * (c->start + (shared ? tiles : std::max(1.0, tiles)) * c->full);
+    const double one = c->start + (shared ? chain : ceil(chain)) * c->alone;
+    const double us = std::max(all, one) + 0.35 * std::min(all, one);
     if (c->form == SHARED_1 || us < least) {
       best = c->form;
       least = us;
@@ -449,7 +458,9 @@ hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void
     case WAVES_1: return a.dh == 64 ? launch_units<64, 1>(a, o, out, lse, st) : launch_units<128, 1>(a, o, out, lse, st);
     case WAVES_2: return a.dh == 64 ? launch_units<64, 2>(a, o, out, lse, st) : launch_units<128, 2>(a, o, out, lse, st);
     case WAVES_4: return a.dh == 64 ? launch_units<64, 4>(a, o, out, lse, st) : launch_units<128, 4>(a, o, out, lse, st);
-    case SHARED_2: return launch<128, 2>(a, o, heads, out, lse, st);   // (d_head 64 never)
+    case SHARED_2:
+      if (a.dh == 128) return launch<128, 2>(a, o, heads, out, lse, st);
+      [[fallthrough]];
     default: return a.dh == 64 ? launch<64, 1>(a, o, heads, out, lse, st) : launch<128, 1>(a, o, heads, out, lse, st);
   }
 }
