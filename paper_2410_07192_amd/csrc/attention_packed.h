@@ -32,6 +32,11 @@ __device__ __forceinline__ Span queries_of(const PackedRows& p, int r0, int row,
 // value of lane `lane`, as a scalar
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
+// A lane's row sees rows lo .. hi - 1 of a tile of 64 (either may lie outside).  Whether that is a part of the tile, neither all nor
+// nothing of it, and whether row i is not among them (one comparison; length: hi - lo).
+__device__ __forceinline__ bool seen_in_part(int lo, int hi) { return (lo > 0 || hi < 64) && lo < 64 && hi > 0 && lo < hi; }
+__device__ __forceinline__ bool hidden_at(int i, int lo, int length) { return (uint32_t)(i - lo) >= (uint32_t)max(length, 0); }
+
 // sum over the wave, the same in all lanes
 __device__ __forceinline__ int wave_total(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8: lane 15 of each row has its sum

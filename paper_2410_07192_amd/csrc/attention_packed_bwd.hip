@@ -158,6 +158,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
     lds_char_ptr tdO = tQ + TILE;
     const bool masked = q_now < in_lo || q_now + 64 > in_hi;
     const int lo = own.lo - q_now, hi = own.hi - q_now;
+    const bool by_element = __any(seen_in_part(lo, hi));   // of a masked tile; otherwise a lane's key is seen from all of the tile or from none
     bf16x8 fp[4], fds[4];   // P and dS, rounded to bf16 (half a step, 2^-8 of each)
 #pragma unroll
     for (int qs = 0; qs < 2; ++qs) {
@@ -183,10 +184,13 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
         }
       }
       if (masked) {
+        if (by_element) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int q = qs * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-          if (q < lo || q >= hi) aS[r] = aP[r] = 0.f;
+          for (int r = 0; r < 16; ++r)
+            if (hidden_at(qs * 32 + 8 * (r >> 2) + (r & 3), lo - 4 * g, hi - lo)) aS[r] = aP[r] = 0.f;
+        } else if (hi < 64 || lo > 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
         }
       }
 #pragma unroll
@@ -302,6 +306,7 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
     lds_char_ptr tK = (lds_char_ptr)(lds_void_ptr)smem + buf * BUF;
     const bool masked = k0 < in_lo || k0 + 64 > in_hi;
     const int lo = own.lo - k0, hi = own.hi - k0;
+    const bool by_element = __any(seen_in_part(lo, hi));
     bf16x8 fds[4];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
@@ -317,10 +322,13 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 #pragma unroll
       for (int r = 0; r < 16; ++r) aP[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
       if (masked) {
+        if (by_element) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = ks * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-          if (key < lo || key >= hi) aP[r] = 0.f;
+          for (int r = 0; r < 16; ++r)
+            if (hidden_at(ks * 32 + 8 * (r >> 2) + (r & 3), lo - 4 * g, hi - lo)) aP[r] = 0.f;
+        } else if (hi < 64 || lo > 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) aP[r] = 0.f;
         }
       }
 #pragma unroll

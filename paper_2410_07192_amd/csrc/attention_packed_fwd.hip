@@ -75,8 +75,9 @@ struct FwdRows {
     // Most tiles that are masked lie in the block's first sequence and none of its rows of the next one sees them: a lane's row sees all of
     // the tile or nothing of it, and has its reference point or needs none (2048 rows behind 5 others, 16 heads on 2 of 128:
     // 65 us with every such tile masked by element, 52 so).
-    const bool all = own.lo <= k0 && own.hi >= k0 + 64, none = own.hi <= k0 || own.lo >= k0 + 64;
-    if (!fresh && !(masked && __any(!(none || (all && m_ref != -INFINITY))))) {
+    const int lo = own.lo - k0, hi = own.hi - k0;
+    const bool none = masked && (lo > 0 || hi < 64);   // unless the tile is masked by element
+    if (!fresh && !(masked && __any(seen_in_part(lo, hi) || (!none && m_ref == -INFINITY)))) {
       const float tot = exponentials(s, none);
       if (!__any(!(tot <= 128.0f))) {   // (also infinite or NaN)
         l_run += tot;
@@ -85,14 +86,11 @@ struct FwdRows {
       scores(sK, s);
     }
     if (masked) {
-      const int lo = own.lo - k0 - 4 * g, hi = own.hi - k0 - 4 * g;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = ks * 32 + 8 * (r >> 2) + (r & 3);
-          if (key < lo || key >= hi) s[ks][r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (hidden_at(ks * 32 + 8 * (r >> 2) + (r & 3), lo - 4 * g, hi - lo)) s[ks][r] = -INFINITY;
     }
     float mx0 = fmaxf(s[0][0], s[1][0]), mx1 = fmaxf(s[0][1], s[1][1]);
 #pragma unroll
@@ -100,9 +98,9 @@ struct FwdRows {
       mx0 = fmaxf(fmaxf(mx0, s[0][r]), s[1][r]);
       mx1 = fmaxf(fmaxf(mx1, s[0][r + 1]), s[1][r + 1]);
     }
-    float lo, hi;
-    both_halves(fmaxf(mx0, mx1), lo, hi);
-    const float m_new = fmaxf(m_ref, fmaxf(lo, hi) * scale_log2e);
+    float mx_lo, mx_hi;
+    both_halves(fmaxf(mx0, mx1), mx_lo, mx_hi);
+    const float m_new = fmaxf(m_ref, fmaxf(mx_lo, mx_hi) * scale_log2e);
     if (!fresh && __any(m_new > m_ref)) {
       const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_ref - m_new);   // m_ref = -inf: 0
       l_run *= alpha;

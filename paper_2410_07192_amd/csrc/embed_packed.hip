@@ -345,8 +345,11 @@ BwdLayout bwd_layout(int64_t tokens, int64_t S, int64_t d, int64_t V) {
   L.log_wgs = 8;
   while ((((int64_t)GROUP_IDS) << L.log_wgs) < V) ++L.log_wgs;
   L.own = (int32_t)((V + ((int64_t)1 << L.log_wgs) - 1) >> L.log_wgs);
-  L.share = 16;
   L.slices = (int32_t)((d + 511) / 512);
+  // Entries per wave.  Eight are loaded at a time, so few waves are done earlier with eight each, many carry fewer partial sums and read
+  // less about their groups with 16 (549 rows of 512, fp32: 18.6 us with 16, 16.8 with 8; 4000 of 680: 18.9, 17.8; 7250 of 1024:
+  // 45.4, 48.4; 12400 of 400: 27.5, 28.7).  Positions have as many waves as tokens.
+  L.share = (tokens + 15) / 16 * L.slices * 2 < 1280 ? 8 : 16;
   L.shares = (tokens + L.share - 1) / L.share;
   int64_t at = 0;
   auto take = [&](int64_t n) {
