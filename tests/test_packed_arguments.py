@@ -96,3 +96,17 @@ def test_embedding_workspace():
 
 def test_struct_size_matches_the_header():
     assert C.sizeof(pf.pf_packed_attn) == 64
+
+
+@pytest.mark.parametrize("kw", [dict(ld_q=(1 << 24) + 8), dict(ld_k=(1 << 24) + 8), dict(ld_v=1 << 40), dict(ld_out=(1 << 24) + 8),
+                                dict(tokens=1 << 24, n_heads=16), dict(n_seq=1 << 31), dict(n_heads=1 << 27, n_kv_heads=1 << 27)], ids=str)
+def test_attention_sizes_refused(kw):
+    if kw.get("n_seq", 0) >= 1 << 31:
+        desc = _desc()
+        desc.n_seq = -(1 << 31)      # what a 32-bit field makes of it
+    else:
+        desc = _desc(**kw)
+    for call in (_fwd, _bwd):
+        with pytest.raises(pf.PipeFillError) as e:
+            call(desc)
+        assert e.value.code == pf.PF_ERR_ARG
