@@ -70,10 +70,11 @@ struct BwdArgs {
 };
 
 // ---- dK, dV ------------------------------------------------------------------------------------------------------------------
-// Workgroup `unit`; whether a result is infinite or NaN.  smem: two buffers; s_span: two ints.
-template <int DH, bool CAREFUL>
+// Workgroup `unit`; whether a result is infinite or NaN.  smem: two buffers; s_span: two ints.  WANT: 1 dV, 2 dK, 3 both.
+template <int DH, int WANT, bool CAREFUL>
 __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr int KS = DH / 16, DT = DH / 32, ROWB = DH * 2, TILE = 64 * ROWB;
+  constexpr bool DV = WANT & 1, DK = WANT & 2;
   constexpr int BUF = 2 * TILE + 512;   // Q tile | dO tile | lse (log2 units) of the 64 queries | D
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
   const int n_kv = a.o.h / a.o.group, T = a.o.rows.tokens;
@@ -82,7 +83,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   const int hk = (int)((uint32_t)unit % per) % n_kv, split = (int)((uint32_t)unit % per) / n_kv;
   const int k_blk = block_in_order(a.o.rows, (int)((uint32_t)unit / per), a.k_blocks, 7, a.o.causal, true, a.at_once & 1) * 128;
   const int key = k_blk + wave * 32 + lr;
-  bf16x8 fk[KS], fv[KS];
+  bf16x8 fk[KS], fv[DK ? KS : 1];
   {
     const int row = min(key, T - 1);
     const bf16_t* pk = a.o.k + (int64_t)row * a.o.ld_k + hk * DH + g * 8;
@@ -90,7 +91,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
       fk[kk] = as_bf16x8(*(const uint4*)(pk + kk * 16));
-      fv[kk] = as_bf16x8(*(const uint4*)(pv + kk * 16));
+      if constexpr (DK) fv[kk] = as_bf16x8(*(const uint4*)(pv + kk * 16));
     }
   }
   const Span own = queries_of(a.o.rows, k_blk + wave * 32, key, a.o.causal);
@@ -117,9 +118,12 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
   };
   int t_off[DT][2];
   tr_offsets<DH>(lane, t_off);
-  f32x16 accK[DT], accV[DT];
+  f32x16 accK[DK ? DT : 1], accV[DV ? DT : 1];
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) asm volatile("" ::"v"(fk[kk]), "v"(fv[kk]));   // waited for here, once
+  for (int kk = 0; kk < KS; ++kk) {   // waited for here, once
+    asm volatile("" ::"v"(fk[kk]));
+    if constexpr (DK) asm volatile("" ::"v"(fv[kk]));
+  }
   // the tiles of one head after the other; this split's part of them
   const int64_t all = (int64_t)tiles * a.o.group;
   const int64_t first = all * split / a.splits;
@@ -127,7 +131,10 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) accK[i][r] = accV[i][r] = 0.f;
+    for (int r = 0; r < 16; ++r) {
+      if constexpr (DK) accK[i][r] = 0.f;
+      if constexpr (DV) accV[i][r] = 0.f;
+    }
   float ld = 0.f;
   int hd = hk * a.o.group, q0 = q_begin;
   if (steps > 0) {
@@ -170,7 +177,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
         const int r = qs * 32 + lr;
         const int o = r * ROWB + (((kk * 2 + g) ^ SwzBoth<DH>::of(r)) << 4);
         aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sQ + o)), fk[kk], aS, 0, 0, 0);
-        aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
+        if constexpr (DK) aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
       }
 #pragma unroll
       for (int rg = 0; rg < 4; ++rg) {
@@ -180,7 +187,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
         for (int j = 0; j < 4; ++j) {
           const int r = rg * 4 + j;
           aS[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, -L4[j]));
-          aP[r] = aS[r] * (aP[r] - D4[j]);
+          if constexpr (DK) aP[r] = aS[r] * (aP[r] - D4[j]);
         }
       }
       if (masked) {
@@ -195,51 +202,50 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
       }
 #pragma unroll
       for (int i = 2 * qs; i < 2 * qs + 2; ++i) {
-        fp[i] = as_operand(aS, i);
-        fds[i] = as_operand(aP, i);
+        if constexpr (DV) fp[i] = as_operand(aS, i);
+        if constexpr (DK) fds[i] = as_operand(aP, i);
         if (CAREFUL && masked) continue;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp[i], accV[dt], 0, 0, 0);
-          accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds[i], accK[dt], 0, 0, 0);
+          if constexpr (DV) accV[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tdO, t_off[dt][0], t_off[dt][1], i), fp[i], accV[dt], 0, 0, 0);
+          if constexpr (DK) accK[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_tr<ROWB>(tQ, t_off[dt][0], t_off[dt][1], i), fds[i], accK[dt], 0, 0, 0);
         }
       }
     }
     if (CAREFUL && masked) {
       auto off = [&](int dt, int r) { return t_off[dt][r]; };
-      add_with_care<DH>(accV, fp, tdO, off, lo, hi);
-      add_with_care<DH>(accK, fds, tQ, off, lo, hi);
+      if constexpr (DV) add_with_care<DH>(accV, fp, tdO, off, lo, hi);
+      if constexpr (DK) add_with_care<DH>(accK, fds, tQ, off, lo, hi);
     }
   }
-  const bool odd = !CAREFUL && __syncthreads_or((not_finite<DT>(accK) || not_finite<DT>(accV)) && own.lo < own.hi);
-  if (own.lo >= own.hi) return odd;
-  if (a.partial == nullptr) {
-    bf16_t* pk = a.dk + (int64_t)key * a.o.ld_k + hk * DH;
-    bf16_t* pv = a.dv + (int64_t)key * a.o.ld_v + hk * DH;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int rg = 0; rg < 4; ++rg) {
-        float vk[4], vv[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          vk[j] = accK[dt][rg * 4 + j] * a.o.scale;
-          vv[j] = accV[dt][rg * 4 + j];
-        }
-        store4(pk + dt * 32 + rg * 8 + g * 4, vk);
-        store4(pv + dt * 32 + rg * 8 + g * 4, vv);
-      }
-  } else {
-    float* pk = a.partial + ((int64_t)split * 2 * T + key) * (n_kv * DH) + hk * DH;
-    float* pv = pk + (int64_t)T * (n_kv * DH);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int rg = 0; rg < 4; ++rg) {
-        *(f32x4*)(pk + dt * 32 + rg * 8 + g * 4) = f32x4{accK[dt][rg * 4], accK[dt][rg * 4 + 1], accK[dt][rg * 4 + 2], accK[dt][rg * 4 + 3]};
-        *(f32x4*)(pv + dt * 32 + rg * 8 + g * 4) = f32x4{accV[dt][rg * 4], accV[dt][rg * 4 + 1], accV[dt][rg * 4 + 2], accV[dt][rg * 4 + 3]};
-      }
+  bool odd = false;
+  if constexpr (!CAREFUL) {
+    if constexpr (DK) odd = not_finite<DT>(accK);
+    if constexpr (DV) odd = odd || not_finite<DT>(accV);
+    odd = __syncthreads_or(odd && own.lo < own.hi);
   }
+  if (own.lo >= own.hi) return odd;
+  auto store = [&](const f32x16* acc, bf16_t* dst, int64_t ld, int64_t part, float scale) {
+    if (a.partial == nullptr) {
+      bf16_t* row = dst + (int64_t)key * ld + hk * DH;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg) {
+          const float v[4] = {acc[dt][rg * 4] * scale, acc[dt][rg * 4 + 1] * scale, acc[dt][rg * 4 + 2] * scale, acc[dt][rg * 4 + 3] * scale};
+          store4(row + dt * 32 + rg * 8 + g * 4, v);
+        }
+    } else {
+      float* row = a.partial + (part * T + key) * (n_kv * DH) + hk * DH;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg)
+          *(f32x4*)(row + dt * 32 + rg * 8 + g * 4) = f32x4{acc[dt][rg * 4], acc[dt][rg * 4 + 1], acc[dt][rg * 4 + 2], acc[dt][rg * 4 + 3]};
+    }
+  };
+  if constexpr (DK) store(accK, a.dk, a.o.ld_k, 2 * split, a.o.scale);
+  if constexpr (DV) store(accV, a.dv, a.o.ld_v, 2 * split + 1, 1.0f);
   return odd;
 }
 
@@ -357,21 +363,29 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
   return odd;
 }
 
-// Both passes in one launch (WHAT 3: the dK/dV workgroups first, they are the longer ones), so that few workgroups of one do not leave
-// the card idle; or one of them (1 dK/dV, 2 dQ).
-template <int DH, int WHAT>
-__global__ __launch_bounds__(256, DH == 64 || WHAT == 2 ? 2 : 1) void packed_bwd_bf16_kernel(BwdArgs a) {
+// Both passes in one launch, the dK/dV workgroups first, they are the longer ones.  d_head 128: dK and dV come from workgroups of their own
+// (PAIR), which compute the scores twice but have half the sums each, so that two waves fit a SIMD and one's matrix products run beside the
+// other's exponentials (PF_FIG).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
+template <int DH, bool CAREFUL>
+__device__ __forceinline__ bool block(const BwdArgs& a, int unit, char* smem, int* s_span) {
+  constexpr bool PAIR = DH == 128;
+  const int k_blocks = PAIR ? (a.k_units + 7) / 8 * 16 : a.k_units;
+  if (unit >= k_blocks) return dq_block<DH, CAREFUL>(a, unit - k_blocks, smem, s_span);
+  if constexpr (PAIR) {
+    const int k = unit / 16 * 8 + unit % 8;
+    if (k >= a.k_units) return false;
+    return unit & 8 ? dkv_block<DH, 1, CAREFUL>(a, k, smem, s_span) : dkv_block<DH, 2, CAREFUL>(a, k, smem, s_span);
+  } else {
+    return dkv_block<DH, 3, CAREFUL>(a, unit, smem, s_span);
+  }
+}
+template <int DH>
+__global__ __launch_bounds__(256, 2) void packed_bwd_bf16_kernel(BwdArgs a) {
   extern __shared__ __align__(16) char dyn_smem[];
   __shared__ int s_span[2];
-  const int unit = (int)blockIdx.x + (WHAT == 2 ? a.k_units : 0);
-  const bool is_k = WHAT == 1 || (WHAT == 3 && unit < a.k_units);
-  bool odd;
-  if (is_k) odd = dkv_block<DH, false>(a, unit, dyn_smem, s_span);
-  else odd = dq_block<DH, false>(a, unit - a.k_units, dyn_smem, s_span);
-  if (odd) {
+  if (block<DH, false>(a, (int)blockIdx.x, dyn_smem, s_span)) {
     __syncthreads();
-    if (is_k) dkv_block<DH, true>(a, unit, dyn_smem, s_span);
-    else dq_block<DH, true>(a, unit - a.k_units, dyn_smem, s_span);
+    block<DH, true>(a, (int)blockIdx.x, dyn_smem, s_span);
   }
 }
 
@@ -418,29 +432,14 @@ BwdArgs plan_of(const PackedAttn& a) {
   b.at_once = (b.k_units <= (a.dh == 64 ? 512 : 256) ? 1 : 0) | (b.q_units <= 512 ? 2 : 0);
   return b;
 }
-// Whether both passes are one launch.  d_head 64: always, they use as many registers.  d_head 128: dQ then runs with one wave per SIMD as
-// dK/dV does, not two, which counts where its tiles fill the card many times over (us apart / together: 24 heads on 8, 6600 rows of 24
-// sequences 267 / 250, 15 on 15, 27359 rows of 120 621 / 656, 16 on 2, 8969 rows of 3 630 / 662; 18 on 6, 150 rows 36 / 25).
-bool together(const PackedAttn& a, const BwdArgs& b) { return a.dh == 64 || b.q_units * (rows_met(a) / 64 + 0.5) < 10000; }
-
-template <int DH, int WHAT>
-hipError_t launch_passes(const BwdArgs& b, hipStream_t st) {
-  constexpr int lds = WHAT == 2 ? 2 * 2 * 64 * DH * 2 : 2 * (2 * 64 * DH * 2 + 512);
-  hipError_t e = allow_lds((const void*)packed_bwd_bf16_kernel<DH, WHAT>, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_bwd_bf16_kernel<DH, WHAT>), dim3((unsigned)((WHAT & 1 ? b.k_units : 0) + (WHAT & 2 ? b.q_units : 0))), dim3(256), lds, st, b);
-  return hipGetLastError();
-}
-
 template <int DH>
 hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
-  hipError_t e;
-  if (together(a, b)) {
-    e = launch_passes<DH, 3>(b, st);
-  } else {
-    e = launch_passes<DH, 1>(b, st);
-    if (e == hipSuccess) e = launch_passes<DH, 2>(b, st);
-  }
+  constexpr int lds = 2 * (2 * 64 * DH * 2 + 512);
+  hipError_t e = allow_lds((const void*)packed_bwd_bf16_kernel<DH>, lds);
+  if (e != hipSuccess) return e;
+  const int k_blocks = DH == 128 ? (b.k_units + 7) / 8 * 16 : b.k_units;
+  hipLaunchKernelGGL(packed_bwd_bf16_kernel<DH>, dim3((unsigned)(k_blocks + b.q_units)), dim3(256), lds, st, b);
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   return b.splits > 1 ? packed_join(a, b.partial, b.splits, b.dk, b.dv, st) : hipSuccess;
 }
