@@ -3,14 +3,17 @@
 //   P = exp(scale S - lse), dP = dO V^T, dS = P (dP - D), D = rowsum(dO O)
 //   dV = P^T dO, dK = scale dS^T Q (both summed over the query heads of a group), dQ = scale dS K
 //
-// Two launches that each own their results (no atomics):
+// Two passes in one launch that each own their results (no atomics):
 //  * dK/dV: a workgroup has 128 keys of a K/V head, a wave 32 of them with K and V as "B" operands in registers, and walks the
 //    tiles of 64 queries of the group's heads.  S = Q K^T and dP = dO V^T put one key and 32 of a tile's 64 queries into a lane:
 //    the "B" operands of dV^T += dO^T P and dK^T += Q^T dS, whose "A" operands come out of the same row-major tiles by the
 //    transposing LDS load.  Where keys and K/V heads are too few for the card, the tiles are dealt out to several workgroups, whose
 //    fp32 sums one more launch adds up.
 //  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
-// Tiles go global -> LDS directly, one tile ahead.  Rows of other sequences: see attention_packed.h.  A workgroup whose results
+// Tiles go global -> LDS directly, one tile ahead.  Bound by what a SIMD issues: matrix products, exponentials and LDS reads take about as
+// long each (seven products of 2 T^2 d_head per head and pass where the formulas have five: S and dP in both passes), and two waves
+// overlap them in part.  d_head 64, 16 heads on 4, one sequence of 8192: 494 us, 0.97 PFLOP/s of products; d_head 128: see below.
+// D = rowsum(dO O) comes from a launch before (5 us at 5000 rows of 16 heads of 64).  Rows of other sequences: see attention_packed.h.  A workgroup whose results
 // hold an infinity or NaN, which rows hidden from them may have brought in, does them again with care, as a second stretch of code behind the first
 // (woven into the first it cost that one registers: dK/dV of d_head 128 took 1880 us instead of 780).
 #include "attention_packed.h"
@@ -365,7 +368,7 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 
 // Both passes in one launch, the dK/dV workgroups first, they are the longer ones.  d_head 128: dK and dV come from workgroups of their own
 // (PAIR), which compute the scores twice but have half the sums each, so that two waves fit a SIMD and one's matrix products run beside the
-// other's exponentials (PF_FIG).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
+// other's exponentials (8 sequences of 1024, 16 heads on 4: 199 us, 241 with both in one workgroup; 20 of 300, 16 heads: 139, 186).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
 template <int DH, bool CAREFUL>
 __device__ __forceinline__ bool block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr bool PAIR = DH == 128;
@@ -397,12 +400,12 @@ double rows_met(const PackedAttn& a) {
 
 // Parts of a block's tiles in dK/dV: the number with the least estimated time.  A workgroup takes `start` and `tile` us per tile of 64
 // queries; either the card's `slots` are full, or the longest block's chain counts (its sequence `longest` times the average);
-// with parts, their fp32 sums go through memory at 4 TB/s in `join` us more.  Fitted to 160 drawn sizes with 1 to 12 parts (MI355X):
-// 2.4 % off the best number on average, 24 % at most (one part everywhere: 45 %).  16 heads of 128 on 2 K/V heads, 8969 rows: 1606 us
-// with one part, 660 with four; 12 on 4, 5750 rows: 247 and 157 (two).
+// with parts, their fp32 sums go through memory at 4 TB/s in `join` us more.  Fitted to 350 sizes with 1 to 16 parts (MI355X):
+// 3 % off the best number on average, 33 % at most (one part everywhere: 37 %).  us with 1 / 2 / 4 / 8 / 16 parts: 16 heads of 128
+// on 2, 8114 rows of 2 sequences 1172 / 692 / 591 / 610 / 669; 16 of 64 on 4, 4680 rows of 8: 207 / 119 / 84 / 101 / 130.
 int splits_of(const PackedAttn& a) {
   struct Cost { double start, tile, slots, join, longest; };
-  const Cost c = a.dh == 64 ? Cost{3, 1.6, 256, 4, 2.5} : Cost{10, 2.2, 192, 2, 1.5};
+  const Cost c = a.dh == 64 ? Cost{3.07, 1.2, 207, 2.37, 1.93} : Cost{13.2, 1.55, 155, 2.63, 1.83};
   const double units = (double)((a.tokens + 127) / 128 * a.h_kv), group = (double)(a.h / a.h_kv), length = (double)a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
   const double most = a.n_seq > 1 ? std::min((double)a.tokens, c.longest * length) : length;
   const double tiles = group * ((rows_met(a) + 128) / 64 + 0.5), chain = group * ((most + 128) / 64 + 0.5);
