@@ -175,6 +175,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
       f32x16 aS, aP;
 #pragma unroll
       for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(1);   // the SIMD's other wave fills the gaps (1081 -> 1023 us at 8192 rows, 16 heads on 4; d_head 64: 483 -> 501)
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const int r = qs * 32 + lr;
@@ -182,6 +183,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
         aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sQ + o)), fk[kk], aS, 0, 0, 0);
         if constexpr (DK) aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sdO + o)), fv[kk], aP, 0, 0, 0);
       }
+      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int rg = 0; rg < 4; ++rg) {
         const int qi = qs * 32 + 8 * rg + 4 * g;
@@ -322,12 +324,14 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
       f32x16 aS, aP;
 #pragma unroll
       for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
+      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const int r = ks * 32 + lr, c = kk * 2 + g;
         aS = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sK + r * ROWB + ((c ^ SwzBoth<DH>::of(r)) << 4))), fq[kk], aS, 0, 0, 0);
         aP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*(const uint4*)(sV + r * ROWB + ((c ^ swz_row<DH>(r)) << 4))), fd[kk], aP, 0, 0, 0);
       }
+      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) aP[r] = __builtin_amdgcn_exp2f(fmaf(aS[r], a.scale_log2e, neg_l)) * (aP[r] - D);
       if (masked) {
@@ -368,7 +372,8 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 
 // Both passes in one launch, the dK/dV workgroups first, they are the longer ones.  d_head 128: dK and dV come from workgroups of their own
 // (PAIR), which compute the scores twice but have half the sums each, so that two waves fit a SIMD and one's matrix products run beside the
-// other's exponentials (8 sequences of 1024, 16 heads on 4: 199 us, 241 with both in one workgroup; 20 of 300, 16 heads: 139, 186).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
+// other's exponentials (8 sequences of 1024, 16 heads on 4: 199 us, 241 with both in one workgroup; 20 of 300, 16 heads: 139, 186; d_head 64
+// has room for both: 8192 rows 483 us so, 594 apart at three waves a SIMD).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
 template <int DH, bool CAREFUL>
 __device__ __forceinline__ bool block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr bool PAIR = DH == 128;
