@@ -482,7 +482,8 @@ hipError_t fwd(const PackedAttn& a, const void* q, const void* k, const void* v,
   return hipGetLastError();
 }
 // Splits of a block's tiles in dK/dV: as many as fill the card, four tiles (one a wave) to each or more if sequences were all as long as
-// they are on average.  (4 heads on 2 of 64, 262 fp32 rows of 4 sequences: 18 blocks of 10 tiles; 36 us with one split and a launch for each pass, 20 with 3 and one launch; 16 of 64 and 4096 rows: 914, 841.)
+// they are on average.  (us in one launch, and with one split and a launch for each pass: 262 rows, 4 heads on 2 of 64, one sequence
+// 22, 65 (three splits), four 20, 36 (one); 512 rows, 4 heads of 128 45, 100 (three); 4096 rows, 16 heads of 64 841, 914 (one).)
 int splits_f32(const PackedAttn& a) {
   const int64_t units = (a.tokens + 31) / 32 * a.h_kv, length = a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
   const int64_t tiles = ((a.causal ? length / 2 : length) + 63) / 32 * (a.h / a.h_kv);
