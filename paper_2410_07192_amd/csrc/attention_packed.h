@@ -32,9 +32,13 @@ __device__ __forceinline__ Span queries_of(const PackedRows& p, int r0, int row,
 // value of lane `lane`, as a scalar
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
-// A lane's row sees rows lo .. hi - 1 of a tile of 64 (either may lie outside).  Whether that is a part of the tile, neither all nor
-// nothing of it, and whether row i is not among them (one comparison; length: hi - lo).
-__device__ __forceinline__ bool seen_in_part(int lo, int hi) { return (lo > 0 || hi < 64) && lo < 64 && hi > 0 && lo < hi; }
+// A lane's row sees rows lo .. hi - 1 of a tile of 64 (either may lie outside): all of the tile; a part of it, neither all nor nothing;
+// and whether row i is not among them (one comparison; length: hi - lo).  (Without short circuits: these are lane masks, not branches.)
+__device__ __forceinline__ bool seen_as_a_whole(int lo, int hi) { return (lo <= 0) & (hi >= 64); }
+__device__ __forceinline__ bool seen_in_part(int lo, int hi) {
+  const bool all = seen_as_a_whole(lo, hi), some = max(lo, 0) < min(hi, 64);
+  return some & !all;
+}
 __device__ __forceinline__ bool hidden_at(int i, int lo, int length) { return (uint32_t)(i - lo) >= (uint32_t)max(length, 0); }
 
 // sum over the wave, the same in all lanes

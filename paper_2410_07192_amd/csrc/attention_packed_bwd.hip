@@ -200,7 +200,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (hidden_at(qs * 32 + 8 * (r >> 2) + (r & 3), lo - 4 * g, hi - lo)) aS[r] = aP[r] = 0.f;
-        } else if (hi < 64 || lo > 0) {
+        } else if (!seen_as_a_whole(lo, hi)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
         }
@@ -339,7 +339,7 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 #pragma unroll
           for (int r = 0; r < 16; ++r)
             if (hidden_at(ks * 32 + 8 * (r >> 2) + (r & 3), lo - 4 * g, hi - lo)) aP[r] = 0.f;
-        } else if (hi < 64 || lo > 0) {
+        } else if (!seen_as_a_whole(lo, hi)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) aP[r] = 0.f;
         }

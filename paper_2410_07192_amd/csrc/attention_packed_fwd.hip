@@ -64,8 +64,7 @@ struct FwdRows {
         s[ks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fk), fq[kk], s[ks], 0, 0, 0);
       }
   }
-  __device__ __forceinline__ float exponentials(f32x16* s, bool none = false) const {   // their sum; none: of keys that the row does not see
-    const float neg_m = none ? -INFINITY : m_ref == -INFINITY ? 0.f : -m_ref;
+  __device__ __forceinline__ float exponentials(f32x16* s, float neg_m) const {   // their sum
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -79,12 +78,11 @@ struct FwdRows {
   // Scores of the tile at key k0 into probabilities.  masked: not every row sees every key; fresh: nothing has been added yet.
   __device__ __forceinline__ void probabilities(const char* sK, f32x16* s, int k0, bool masked, bool fresh) {
     // Most tiles that are masked lie in the block's first sequence and none of its rows of the next one sees them: a lane's row sees all of
-    // the tile or nothing of it, and has its reference point or needs none (2048 rows behind 5 others, 16 heads on 2 of 128:
-    // 65 us with every such tile masked by element, 52 so).
+    // the tile or nothing of it (2048 rows behind 5 others, 16 heads on 2 of 128: 65 us with every such tile masked by element, 52 so).
+    // A row that has met no score but -inf yet has no reference point: its sum is infinite or NaN here, and the tile is done again.
     const int lo = own.lo - k0, hi = own.hi - k0;
-    const bool none = masked && (lo > 0 || hi < 64);   // unless the tile is masked by element
-    if (!fresh && !(masked && __any(seen_in_part(lo, hi) || (!none && m_ref == -INFINITY)))) {
-      const float tot = exponentials(s, none);
+    if (!fresh && !(masked && __any(seen_in_part(lo, hi)))) {
+      const float tot = exponentials(s, seen_as_a_whole(lo, hi) ? -m_ref : -INFINITY);
       if (!__any(!(tot <= 128.0f))) {   // (also infinite or NaN)
         l_run += tot;
         return;
@@ -116,7 +114,7 @@ struct FwdRows {
         for (int r = 0; r < 16; ++r) accO[i][r] *= alpha;
     }
     m_ref = m_new;
-    l_run += exponentials(s);
+    l_run += exponentials(s, m_ref == -INFINITY ? 0.f : -m_ref);
   }
   // O^T += V^T P^T.  P is rounded to bf16 (half a step, 2^-8 of each), its sum is not.
   __device__ __forceinline__ int v_off(int dt) const { return ((dt & 1) ? v_off1 : v_off0) + (dt >> 1) * 128; }

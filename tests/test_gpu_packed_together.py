@@ -14,7 +14,7 @@ from test_gpu_packed_attention import Case, U16, U32, _mods     # noqa: E402
 
 # Lengths, heads, K/V heads, d_head, causal.  With the sizes of test_gpu_packed_attention these reach every form of the forward (tiles
 # shared by the waves of a workgroup, keys in one or two parts; independent waves, 1, 2 or 4 to a block) for both d_head, and the
-# backward in one part and several, its passes in one launch and apart.
+# backward in one part and several.
 FORMS = [
     ([200] * 20, 12, 12, 128, True),                # shared tiles
     ([2000], 12, 12, 128, False),                   # shared tiles in two parts
@@ -22,7 +22,12 @@ FORMS = [
     ([150, 250] * 10, 8, 8, 64, True),              # two waves
     ([40, 300, 1, 120] * 10, 8, 2, 128, True),
     ([700, 900], 16, 16, 64, False),
-    ([2400], 16, 2, 128, False),                    # passes apart
+    ([2400], 16, 2, 128, False),
+    ([1] * 190, 48, 16, 128, True),                 # one wave, d_head 128
+    ([60] * 12, 48, 16, 128, True),
+    ([3] * 51, 36, 12, 128, False),                 # two waves
+    ([323], 48, 12, 128, False),                    # shared tiles in two parts
+    ([33, 40] * 20, 24, 8, 64, False),              # one wave, d_head 64
 ]
 
 
@@ -304,3 +309,34 @@ def test_boundaries_out_of_order_or_range_stay_inside_the_buffers(start, dtype, 
         for t in (out, g):
             assert (t[:pad] == 3.0).all() and (t[-pad:] == 3.0).all()
         assert (lse[:pad] == 3.0).all() and (lse[-pad:] == 3.0).all() and (ws[n:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("dtype,h,kv,dh,lens", [("bf16", 2, 1, 64, [300, 90, 129]), ("bf16", 2, 1, 128, [300, 90, 129]), ("f32", 2, 1, 64, [300, 90]),
+                                                ("bf16", 12, 12, 128, [200] * 20), ("bf16", 8, 8, 64, [90, 110] * 30), ("bf16", 8, 8, 64, [150, 250] * 10)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("none", [64, 70, 128])
+def test_scores_of_minus_infinity_before_any_other(dtype, h, kv, dh, lens, causal, none):
+    """The first keys of every sequence score -inf: they have probability 0, and the softmax takes its maximum from those that follow, near
+    0 or far below.  P and the result are rounded (2^-8 each for bf16), the exponentials and sums of at most 300 keys by 300 2^-24."""
+    def edit(c):
+        c.q[:] = 0
+        c.q[:, :, 0] = 1
+        c.k[:, :, 0] = -np.abs(c.k[:, :, 0])
+        for i, (a, b) in enumerate(zip(c.start[:-1], c.start[1:])):
+            c.k[a:b, :, 0] -= 2000 * (i % 2)
+            c.k[a:min(a + none, b), :, 0] = -np.inf
+
+    c = Case(dtype, lens, h, kv, dh, causal, first=3, seed=7, edit=edit)
+    o, lse = c.forward()
+    r = (2 * U16 if dtype == "bf16" else 0) + 300 * U32 + 1e-5
+    for a, b in list(opk.spans(c.start))[:4]:
+        s = c.k[a:b, :, 0].astype(np.float64) / np.sqrt(dh)
+        for i in range(h):
+            j = i // (h // kv)
+            for row in range(none, b - a, 17):
+                x, v = (s[:row + 1, j], c.v[a:a + row + 1, j]) if causal else (s[:, j], c.v[a:b, j])
+                top = x.max()
+                p = np.exp(x - top)
+                want, mag = (p @ v) / p.sum(), (p @ np.abs(v)) / p.sum()
+                assert (np.abs(o[a + row, i] - want) <= r * mag).all(), (a, i, row)
+                assert abs(lse[i, a + row] - (top + np.log(p.sum()))) <= 1e-5 + 4 * U32 * abs(top), (a, i, row)
