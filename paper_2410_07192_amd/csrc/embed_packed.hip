@@ -12,12 +12,13 @@
 //      ids itself, counts those of lower workgroups for its place in the order, and orders its own with a counter per wave and id:
 //      no communication between workgroups.
 //      Positions need no search: the rows before position p's are sum over sequences of min(length, p).
+//      Other workgroups clear the last rows of a large token table meanwhile.
 //   2. embed_sum_kernel adds up the grouped rows, a fixed number of them per wave however they are spread over the groups.  A
 //      group inside a wave's share goes to its gradient row at once, the sums of groups that go beyond to the workspace.
-//      Other waves clear the rows of the tables that no row of dx belongs to.
+//      Other waves clear the rest of the rows that no row of dx belongs to.
 //   3. embed_join_kernel adds those partial sums up in order.
-// Large tables are bound by writing the gradient (7250 rows of 1024, bf16, into 50257 rows: 9.5 + 31.6 + 4.4 us; the second launch
-// writes 6.5 TB/s), small ones by the three launches after each other (549 rows of 512, fp32, into 10007: 5.4 + 7.8 + 3.9).
+// Large tables are bound by writing the gradient (7250 rows of 1024, bf16, into 50257 rows: 54 us for 206 MB of it and 15 MB of dx read
+// twice), small ones by the three launches after each other (549 rows of 512, fp32, into 10007: 5.4 + 7.8 + 3.9).
 #include "packed.h"
 #include "pf_device.h"
 #include "pf_kernels.h"
@@ -84,12 +85,19 @@ struct Grouped {
 constexpr int GROUP_THREADS = 1024, GROUP_WAVES = 16, GROUP_IDS = 1000;   // ids a workgroup can own (LDS: 64 bytes each, 64 KiB in all)
 
 __global__ __launch_bounds__(GROUP_THREADS) void embed_group_kernel(const int32_t* __restrict__ ids, PackedRows p, Grouped by_id, Grouped by_pos,
-                                                                    int32_t log_wgs, int32_t own) {
+                                                                    int32_t log_wgs, int32_t own, int32_t pos_wgs, int32_t d, int32_t id_cleared) {
   extern __shared__ int32_t dyn_cnt[];   // [wave][own]
   __shared__ int32_t s_below[GROUP_WAVES], s_sum[GROUP_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint64_t before = ((uint64_t)1 << lane) - 1;   // lanes below this one
   const int T = p.tokens, wgs = 1 << log_wgs;
+  if ((int)blockIdx.x >= wgs + pos_wgs) {   // the table's last rows: zeros, whether a row of dx belongs to them or not
+    const int64_t n = (int64_t)(by_id.n_keys - id_cleared) * d, all = (int64_t)(gridDim.x - wgs - pos_wgs) * GROUP_THREADS;
+    float* to = by_id.grad + (int64_t)id_cleared * d;
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t i = (int64_t)((int)blockIdx.x - wgs - pos_wgs) * GROUP_THREADS + tid; i < n / 4; i += all) store4(to + i * 4, zero);
+    return;
+  }
   if ((int)blockIdx.x >= wgs) {   // positions: one per wave
     const int at = ((int)blockIdx.x - wgs) * GROUP_WAVES + wave;
     if (at >= by_pos.n_keys) return;
@@ -209,6 +217,7 @@ struct SumPlan {
   int32_t share;                    // entries per wave, at most 64
   int32_t slices;                   // of 512 columns
   int64_t id_end, pos_end, id_zero_end, pos_zero_end;
+  int32_t id_cleared;               // token rows from here on are zeros already
 };
 constexpr int ZERO_RUN = 16;
 
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T* __restrict__ dx
   if (item >= plan.pos_end) {
     item -= item < plan.id_zero_end ? plan.pos_end : plan.id_zero_end;
     const int64_t k0 = item * ZERO_RUN;
-    const bool none = lane < ZERO_RUN && k0 + lane < G.n_keys && G.count[k0 + lane] == 0;
+    const bool none = lane < ZERO_RUN && k0 + lane < (tokens_ ? plan.id_cleared : G.n_keys) && G.count[k0 + lane] == 0;
     uint64_t left = __ballot(none);
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
     while (left) {
@@ -401,14 +410,20 @@ hipError_t embed_packed_bwd(int32_t dtype, const void* dx, const int32_t* ids, c
   Grouped by_id{ints(L.id_row), ints(L.id_key), ints(L.id_first), ints(L.id_count), ints(L.totals), V, dtok, (float*)(w + L.id_partial), scale};
   Grouped by_pos{ints(L.pos_row), ints(L.pos_key), ints(L.pos_first), ints(L.pos_count), ints(L.totals) + 1, dpos ? S : 0, dpos, (float*)(w + L.pos_partial), 1.0f};
   const int wgs = 1 << L.log_wgs, pos_wgs = dpos ? (S + GROUP_WAVES - 1) / GROUP_WAVES : 0;
-  hipLaunchKernelGGL(embed_group_kernel, dim3((unsigned)(wgs + pos_wgs)), dim3(GROUP_THREADS), (size_t)GROUP_WAVES * L.own * 4, stream, ids, p, by_id, by_pos,
-                     L.log_wgs, L.own);
+  // Grouping leaves the memory idle: of a large table it clears the rows of the second half (rare tokens, where ids go by frequency) beside
+  // it, the few of them that have a gradient are written twice.  (50257 rows of 1024: 46.0 us without, 45.2 / 43.8 / 42.2 / 41.7 / 43.8
+  // with the last 16 / 32 / 64 / 96 / 128 MB; tables of 20 MB and less: no difference.)
+  const int clear_rows = !accumulate && (int64_t)V * d * 4 >= (64 << 20) ? V / 2 : 0;
+  const int id_cleared = V - clear_rows;
+  const int clear_wgs = clear_rows > 0 ? (int)std::min<int64_t>(512, ((int64_t)clear_rows * d / 4 + GROUP_THREADS - 1) / GROUP_THREADS) : 0;
+  hipLaunchKernelGGL(embed_group_kernel, dim3((unsigned)(wgs + pos_wgs + clear_wgs)), dim3(GROUP_THREADS), (size_t)GROUP_WAVES * L.own * 4, stream, ids, p, by_id, by_pos,
+                     L.log_wgs, L.own, pos_wgs, d, id_cleared);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  SumPlan plan{L.share, L.slices, 0, 0, 0, 0};
+  SumPlan plan{L.share, L.slices, 0, 0, 0, 0, id_cleared};
   plan.id_end = L.shares * L.slices;
   plan.pos_end = plan.id_end + (dpos ? L.shares * L.slices : 0);
-  plan.id_zero_end = plan.pos_end + (accumulate ? 0 : ((int64_t)V + ZERO_RUN - 1) / ZERO_RUN);
+  plan.id_zero_end = plan.pos_end + (accumulate ? 0 : ((int64_t)id_cleared + ZERO_RUN - 1) / ZERO_RUN);
   plan.pos_zero_end = plan.id_zero_end + (accumulate || !dpos ? 0 : ((int64_t)S + ZERO_RUN - 1) / ZERO_RUN);
   const dim3 sum_grid((unsigned)((plan.pos_zero_end + 3) / 4)), block(256);
   if (dtype == PF_DTYPE_BF16_) hipLaunchKernelGGL(embed_sum_kernel<bf16_t>, sum_grid, block, 0, stream, (const bf16_t*)dx, by_id, by_pos, plan, (int32_t)tokens, d, accumulate);

@@ -340,3 +340,35 @@ def test_scores_of_minus_infinity_before_any_other(dtype, h, kv, dh, lens, causa
                 want, mag = (p @ v) / p.sum(), (p @ np.abs(v)) / p.sum()
                 assert (np.abs(o[a + row, i] - want) <= r * mag).all(), (a, i, row)
                 assert abs(lse[i, a + row] - (top + np.log(p.sum()))) <= 1e-5 + 4 * U32 * abs(top), (a, i, row)
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("V,d,dtype", [(33001, 520, "f32"), (70000, 256, "bf16")])
+def test_embedding_gradient_of_a_large_table(V, d, dtype, accumulate):
+    """A table of more than 64 MB, whose last rows are cleared in another launch than the first: rows that tokens use and rows that none
+    does, in both parts and at the border.  A row's error: its number of terms times 2^-24 of their magnitudes."""
+    pf, _ = _mods()
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    border = V - V // 2
+    T, S, scale, lens = 700, 600, 1.5, [600, 3, 90]
+    ids = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+    ids[5:9], ids[9:60], ids[60:64] = border - 1, border, V - 1
+    ids[64:70] = 0
+    tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    dx = torch.randn(T, d, device="cuda", generator=gen).to(tt)
+    start = torch.tensor([2] + [2 + sum(lens[:i + 1]) for i in range(3)], device="cuda", dtype=torch.int32)
+    live = slice(2, 2 + sum(lens))
+    dtok, dpos = torch.full((V + 1, d), 0.5, device="cuda"), torch.full((S, d), 0.5, device="cuda")
+    n = pf.pf_op_embed_packed_bwd_workspace(T, S, d, V)
+    ws = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+    pf.pf_op_embed_packed_bwd(pf.PF_DTYPE_BF16 if dtype == "bf16" else pf.PF_DTYPE_F32, dx.data_ptr(), ids.data_ptr(), start.data_ptr(), 3, scale,
+                              dtok.data_ptr(), dpos.data_ptr(), accumulate, ws.data_ptr(), n, T, S, d, V)
+    x, at = dx[live].double(), ids[live].long()
+    want, mag, count = (torch.zeros(V, w, device="cuda", dtype=torch.double) for w in (d, d, 1))
+    want.index_add_(0, at, x * scale)
+    mag.index_add_(0, at, x.abs() * scale)
+    count.index_add_(0, at, torch.ones(len(at), 1, device="cuda", dtype=torch.double))
+    want += 0.5 * accumulate
+    torch.cuda.synchronize()
+    assert (dtok[V] == 0.5).all()
+    assert ((dtok[:V].double() - want).abs() <= (count + 2) * U32 * mag + U32 * accumulate * (count > 0)).all()
