@@ -372,3 +372,19 @@ def test_embedding_gradient_of_a_large_table(V, d, dtype, accumulate):
     torch.cuda.synchronize()
     assert (dtok[V] == 0.5).all()
     assert ((dtok[:V].double() - want).abs() <= (count + 2) * U32 * mag + U32 * accumulate * (count > 0)).all()
+
+
+@pytest.mark.parametrize("lens,h,kv,dh,causal", [f for f in FORMS if len(f[0]) > 1], ids=lambda x: "x".join(map(str, x[:2])) if isinstance(x, list) else str(x))
+def test_values_of_other_sequences_in_every_form(lens, h, kv, dh, causal):
+    """NaN and infinities in every fifth sequence: the others come out as they do without them, to the same tolerance."""
+    def poison(c):
+        for a, b in zip(c.start[1:-1:5], c.start[2::5]):
+            for x in (c.q, c.k, c.v, c.do):
+                x[a:b:3], x[a + 1:b:3], x[a + 2:b:3] = np.nan, np.inf, -np.inf
+
+    good, bad = (Case("bf16", lens, h, kv, dh, causal, first=5, tail=11, seed=h, edit=e) for e in (None, poison))
+    rows = np.ones(good.T, bool)
+    for a, b in zip(good.start[1:-1:5], good.start[2::5]):
+        rows[a:b] = False
+    good.check_forward(bad.forward(), rows)
+    good.check_backward(bad.backward(*good.saved()), rows)
