@@ -184,11 +184,11 @@ __global__ __launch_bounds__(256) void packed_fwd_f32_kernel(PackedQkv<T> a, T* 
     float mq = sM[0][i];
 #pragma unroll
     for (int w = 1; w < NW; ++w) mq = fmaxf(mq, sM[w][i]);
-    float lq = 0.f;   // a query whose scores are all -inf has no softmax: exp(-inf - -inf) makes it NaN
+    float lq = 0.f;   // a query whose scores are all -inf has no softmax: 0 / 0, and log(0) = -inf for lse
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = __expf(sM[w][i] - mq);   // 0 for a wave that met no key of this query
+      const float f = mq == -INFINITY ? 1.f : __expf(sM[w][i] - mq);   // 0 for a wave that met no key of this query
       lq += f * sL[w][i];
       o += *(const f32x4*)&sO[w][i][c] * f;
     }
