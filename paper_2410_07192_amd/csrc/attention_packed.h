@@ -86,6 +86,7 @@ constexpr float LOG2E_P = 1.4426950408889634f;
 // ---- bf16 MFMA kernels ------------------------------------------------------------------------------------------------------
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
+typedef uint16_t v8u __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
 typedef const __attribute__((address_space(3))) char* lds_char_ptr;
@@ -198,8 +199,10 @@ __device__ __forceinline__ bf16x8 as_operand(const f32x16& half, int i) {
 
 // acc[dt] += X^T W for a tile that not every row sees as a whole, with care: 0 (hidden) times an infinity or NaN of X would be
 // NaN, so those go into the product as 0 and are counted apart, over visible rows only: a row of X that is +inf, -inf or NaN
-// counts 1, 2^7 or 2^14 (at most 64 rows: exact in fp32).  w: the "B" operands of the 64 rows' weights, visible rows lo .. hi - 1
-// (of the tile); off(dt, r): byte offsets of the two transposing reads.  Weights of visible rows are > 0, or NaN, or of either sign with a result that is NaN anyway.
+// counts 1, 2^7 or 2^14 (at most 64 rows: exact in fp32), and 2^14 times that where its weight is 0, which makes an infinity NaN as in
+// a tile that is seen as a whole.  A weight below 0 meets no infinity: weights of dS have that sign alone, and an infinite element of K or
+// Q makes its row's scores infinite or NaN, so P is 0 or NaN there.  NaN weights make NaN of the zeros.
+// w: the "B" operands of the 64 rows' weights, visible rows lo .. hi - 1 (of the tile); off(dt, r): byte offsets of the two transposing reads.
 template <int DH, class Off>
 __device__ __forceinline__ void add_with_care(f32x16* acc, const bf16x8* w, lds_char_ptr tile, Off off, int lo, int hi) {
   const int g = (threadIdx.x & 63) >> 5;
@@ -212,24 +215,24 @@ __device__ __forceinline__ void add_with_care(f32x16* acc, const bf16x8* w, lds_
     for (int i = 0; i < 4; ++i) {
       __builtin_amdgcn_sched_barrier(0);   // one step's registers at a time
       const v8s x = __builtin_bit_cast(v8s, read_tr<DH * 2>(tile, off(dt, 0), off(dt, 1), i));
-      v8s clean, mark, seen;
+      v8s clean, mark;
+      const v8u weight = __builtin_bit_cast(v8u, w[i]) & (uint16_t)0x7fff;
+      v8u seen = (uint16_t)0x4680 - __builtin_elementwise_min(weight, v8u(1)) * (uint16_t)0x0700;   // weight 0: 2^14, else 1
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const int row = 16 * i + 8 * (t >> 2) + 4 * g + (t & 3);
         const bool is_odd = (x[t] & 0x7f80) == 0x7f80;
         clean[t] = is_odd ? (short)0 : x[t];
         mark[t] = !is_odd ? (short)0 : (x[t] & 0x7f) ? (short)0x4680 : x[t] < 0 ? (short)0x4300 : (short)0x3f80;   // 2^14, 2^7, 1
-        seen[t] = row >= lo && row < hi ? (short)0x3f80 : (short)0;
+        if (hidden_at(16 * i + 8 * (t >> 2) + (t & 3), lo - 4 * g, hi - lo)) seen[t] = 0;
       }
       acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, clean), w[i], acc[dt], 0, 0, 0);
       odd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, seen), odd, 0, 0, 0);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int n = (int)odd[r];
-      if (n & 0x7f) acc[dt][r] += INFINITY;
-      if ((n >> 7) & 0x7f) acc[dt][r] -= INFINITY;
-      if (n >> 14) acc[dt][r] = NAN;
+      const int n = (int)fminf(odd[r], 16384.f);
+      const bool plus = (n & 0x7f) != 0, minus = (n & 0x3f80) != 0, nan = (n >> 14 != 0) | (plus & minus);
+      acc[dt][r] += nan ? NAN : plus ? INFINITY : minus ? -INFINITY : 0.f;
     }
   }
 }

@@ -44,3 +44,69 @@ def test_a_row_that_sees_only_minus_infinity(dtype, lens, h, kv, dh, shift, caus
     assert (lse[:, a:b] == -np.inf).all()
     assert np.isnan(o[a:b]).all()
     assert np.isfinite(lse[:, 3:a]).all() and np.isfinite(o[3:a]).all()
+
+
+# Sequences of which rows see some tiles in part and some as a whole: what a row gets does not depend on which
+ODD = KERNELS + [("bf16", [64, 128, 320], 4, 2, 64, 0), ("bf16", [64, 128, 320], 4, 2, 128, 0)]
+AT = 20     # a key of every sequence that gets no weight
+
+
+@pytest.mark.parametrize("dtype,lens,h,kv,dh,shift", ODD, ids=name)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("far", [-np.inf, -1e4])
+def test_an_infinite_value_whose_weight_is_zero(dtype, lens, h, kv, dh, shift, causal, far):
+    """A key with a score of -inf, or so low that its weight is 0 in 32 bits, with an infinity in V: 0 times it is NaN, in that column of
+    the rows that see the key."""
+    def edit(c):
+        c.q[:, :, 0] = 1
+        c.k[:, :, 0] = 0
+        c.k[c.start[:-1] + AT, :, 0] = far
+        c.v[c.start[:-1] + AT, :, 5] = np.inf
+
+    c = Case(dtype, lens, h, kv, dh, causal, 3, 2, shift=shift, seed=8, edit=edit)
+    o, lse = c.forward()
+    assert np.isfinite(lse[:, c.live]).all()
+    for a, b in zip(c.start[:-1], c.start[1:]):
+        first = a + AT if causal else a
+        assert np.isnan(o[first:b, :, 5]).all()
+        assert np.isfinite(o[a:first]).all() and np.isfinite(np.delete(o[a:b], 5, axis=2)).all()
+
+
+@pytest.mark.parametrize("dtype,lens,h,kv,dh,shift", ODD, ids=name)
+@pytest.mark.parametrize("causal", [False, True])
+def test_an_infinite_key_whose_weight_is_zero(dtype, lens, h, kv, dh, shift, causal):
+    """A key with an infinity that makes its scores -inf: P and dS are 0, and dQ = dS K is NaN in that column of the rows that see it."""
+    def edit(c):
+        c.q[:, :, 5] = 1
+        c.k[c.start[:-1] + AT, :, 5] = -np.inf
+
+    c = Case(dtype, lens, h, kv, dh, causal, 3, 2, shift=shift, seed=8, edit=edit)
+    o, lse = c.forward()
+    assert np.isfinite(o[c.live]).all() and np.isfinite(lse[:, c.live]).all()
+    dq, dk, dv = c.backward(o, lse)
+    for a, b in zip(c.start[:-1], c.start[1:]):
+        first = a + AT if causal else a
+        assert np.isnan(dq[first:b, :, 5]).all()
+        assert np.isfinite(dq[a:first]).all() and np.isfinite(np.delete(dq[a:b], 5, axis=2)).all()
+        assert np.isfinite(dk[a:b]).all() and np.isfinite(dv[a:b]).all()
+
+
+@pytest.mark.parametrize("dtype,lens,h,kv,dh,shift", ODD, ids=name)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_infinite_gradient_whose_weight_is_zero(dtype, lens, h, kv, dh, shift, causal, sign):
+    """An infinity in dO of every sequence's last row: dV = P^T dO is NaN in that column of the key that the row gives no weight, and
+    that infinity for all others."""
+    def edit(c):
+        c.q[:, :, 0] = 1
+        c.k[:, :, 0] = 0
+        c.k[c.start[:-1] + AT, :, 0] = -np.inf
+        c.do[c.start[1:] - 1, :, 5] = sign * np.inf
+
+    c = Case(dtype, lens, h, kv, dh, causal, 3, 2, shift=shift, seed=8, edit=edit)
+    o, lse = c.forward()
+    dv = c.backward(o, lse)[2]
+    for a, b in zip(c.start[:-1], c.start[1:]):
+        assert np.isnan(dv[a + AT, :, 5]).all()
+        assert (np.delete(dv[a:b, :, 5], AT, axis=0) == sign * np.inf).all()
+        assert np.isfinite(np.delete(dv[a:b], 5, axis=2)).all()
