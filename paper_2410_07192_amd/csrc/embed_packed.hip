@@ -109,11 +109,11 @@ __global__ __launch_bounds__(GROUP_THREADS) void embed_group_kernel(const int32_
         return T;
       }
       begin = min(max(p.start[s], 0), T);
-      return max(min(p.start[s + 1], T) - begin, 0);
+      return max(min(max(p.start[s + 1], 0), T) - begin, 0);
     };
-    int rows_before = 0, begin = 0;
-    for (int s = lane; s < n; s += 64) rows_before += min(length(s, begin), at);
-    for (int o = 32; o > 0; o >>= 1) rows_before += __shfl_xor(rows_before, o, 64);
+    int rows_before = 0, begin = 0;   // at most T, unless sequences overlap: counted no further, so that no sum passes 32 bits
+    for (int s = lane; s < n; s += 64) rows_before = min(rows_before + min(length(s, begin), at), T);
+    for (int o = 32; o > 0; o >>= 1) rows_before = min(rows_before + __shfl_xor(rows_before, o, 64), T);
     int e = rows_before;
     for (int s0 = 0; s0 < n; s0 += 64) {
       const bool has = length(s0 + lane, begin) > at;
@@ -123,12 +123,12 @@ __global__ __launch_bounds__(GROUP_THREADS) void embed_group_kernel(const int32_
         by_pos.row[to] = begin + at;
         by_pos.key[to] = at;
       }
-      e += __popcll(m);
+      e = min(e + __popcll(m), T);
     }
     if (lane == 0) {
-      by_pos.first[at] = min(max(rows_before, 0), T);
-      by_pos.count[at] = min(max(e, 0), T) - min(max(rows_before, 0), T);
-      if (at == by_pos.n_keys - 1) *by_pos.total = min(max(e, 0), T);
+      by_pos.first[at] = rows_before;
+      by_pos.count[at] = e - rows_before;
+      if (at == by_pos.n_keys - 1) *by_pos.total = e;
     }
     return;
   }

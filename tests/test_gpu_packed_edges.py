@@ -110,3 +110,33 @@ def test_an_infinite_gradient_whose_weight_is_zero(dtype, lens, h, kv, dh, shift
         assert np.isnan(dv[a + AT, :, 5]).all()
         assert (np.delete(dv[a:b, :, 5], AT, axis=0) == sign * np.inf).all()
         assert np.isfinite(np.delete(dv[a:b], 5, axis=2)).all()
+
+
+def _overlapping(n, T):
+    """Every second pair of boundaries is a sequence of all T rows: together far longer than the buffer."""
+    return [0, T] * (n // 2) + [0]
+
+
+@pytest.mark.parametrize("start", [[2 ** 31 - 1, -2 ** 31, 5], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [2 ** 31 - 1] * 4, [-2 ** 31] * 4,
+                                   _overlapping(300, 100), [5, -2 ** 31, 60, 2 ** 31 - 1]], ids=lambda s: f"{len(s)}from{s[0]}")
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_embedding_boundaries_at_the_ends_of_32_bits_stay_inside_the_buffers(start, dtype):
+    """Undefined results, but what lies around the buffers keeps its values."""
+    pf, _ = _mods()
+    T, V, S, d, pad, n_seq = 100, 40, 130, 64, 64, len(start) - 1
+    tt, code = (torch.bfloat16, pf.PF_DTYPE_BF16) if dtype == "bf16" else (torch.float32, pf.PF_DTYPE_F32)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    buf = {n: torch.full((rows + 2 * pad, d), 3.0, device="cuda", dtype=t) for n, rows, t in (("x", T, tt), ("dtok", V, torch.float32), ("dpos", S, torch.float32))}
+    at = lambda n: buf[n].data_ptr() + pad * d * buf[n].element_size()
+    src = torch.randn(S, d, device="cuda", generator=gen).to(tt)
+    ids = torch.arange(T, device="cuda", dtype=torch.int32) % V
+    s = torch.tensor(start, dtype=torch.int64).to(torch.int32).cuda()
+    n = pf.pf_op_embed_packed_bwd_workspace(T, S, d, V)
+    ws = torch.full((n + 256,), 0x7f, dtype=torch.uint8, device="cuda")
+    pf.pf_op_embed_packed(code, ids.data_ptr(), src.data_ptr(), src.data_ptr(), s.data_ptr(), n_seq, 1.0, at("x"), T, S, d, V)
+    for accumulate in (0, 1):
+        pf.pf_op_embed_packed_bwd(code, src.data_ptr(), ids.data_ptr(), s.data_ptr(), n_seq, 1.0, at("dtok"), at("dpos"), accumulate, ws.data_ptr(), n, T, S, d, V)
+        torch.cuda.synchronize()
+        for t in buf.values():
+            assert (t[:pad] == 3.0).all() and (t[-pad:] == 3.0).all()
+        assert (ws[n:] == 0x7f).all()
