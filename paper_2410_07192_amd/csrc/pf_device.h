@@ -104,7 +104,8 @@ __device__ __forceinline__ void store8(bf16_t* p, const float v[8]) {
 // flight until the values are needed), and their conversion to float.
 template <typename T> struct Raw8;
 template <> struct Raw8<bf16_t> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
-template <> struct Raw8<float> { typedef float type __attribute__((ext_vector_type(8))); };
+template <> struct Raw8<float> { typedef float type __attribute__((ext_vector_type(8), aligned(16))); };   // as eight bf16 are, not 32
+static_assert(alignof(Raw8<float>::type) == 16 && alignof(Raw8<bf16_t>::type) == 16, "what the callers' pointers are aligned to");
 __device__ __forceinline__ void unpack8(const Raw8<bf16_t>::type& r, float v[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -140,3 +140,37 @@ def test_embedding_boundaries_at_the_ends_of_32_bits_stay_inside_the_buffers(sta
         for t in buf.values():
             assert (t[:pad] == 3.0).all() and (t[-pad:] == 3.0).all()
         assert (ws[n:] == 0x7f).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [24, 520])
+def test_embedding_operands_aligned_to_16_bytes_and_no_more(dtype, d):
+    """The same bits as from allocations of their own, which are aligned to 256 bytes and more."""
+    pf, _ = _mods()
+    tt, code = (torch.bfloat16, pf.PF_DTYPE_BF16) if dtype == "bf16" else (torch.float32, pf.PF_DTYPE_F32)
+    T, V, S, lens = 150, 37, 90, [90, 1, 40]
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    normal = lambda n, t: torch.randn(n, d, device="cuda", generator=gen).to(t)
+    start = torch.tensor([3] + [3 + sum(lens[:i + 1]) for i in range(3)], device="cuda", dtype=torch.int32)
+    ids = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+    operands = {"tok": normal(V, tt), "pos": normal(S, tt), "dx": normal(T, tt), "x": torch.zeros(T, d, device="cuda", dtype=tt),
+                "dtok": torch.ones(V, d, device="cuda"), "dpos": torch.ones(S, d, device="cuda")}
+    n = pf.pf_op_embed_packed_bwd_workspace(T, S, d, V)
+    ws = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+    results = []
+    for by in (0, 16):
+        at = {}
+        for k, t in operands.items():
+            room = torch.zeros(t.numel() + 64, device="cuda", dtype=t.dtype)
+            at[k] = room[by // t.element_size():][:t.numel()].view(t.shape)
+            at[k].copy_(t)
+            assert at[k].data_ptr() % 32 == by % 32
+        p = {k: t.data_ptr() for k, t in at.items()}
+        pf.pf_op_embed_packed(code, ids.data_ptr(), p["tok"], p["pos"], start.data_ptr(), 3, 1.5, p["x"], T, S, d, V)
+        got = [at["x"].clone()]
+        for accumulate in (0, 1):
+            pf.pf_op_embed_packed_bwd(code, p["dx"], ids.data_ptr(), start.data_ptr(), 3, 1.5, p["dtok"], p["dpos"], accumulate, ws.data_ptr(), n, T, S, d, V)
+            got += [at["dtok"].clone(), at["dpos"].clone()]
+        results.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert all(bool(t.any()) for t in results[0])
