@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void embed_packed_kernel(const int32_t* __rest
     idv[i] = __builtin_amdgcn_readlane(id, i);
     plv[i] = __builtin_amdgcn_readlane(place, i);
   }
-  for (int c = part * 512 + lane * 8; c < d; c += parts * 512) {
+  for (uint32_t c = (uint32_t)part * 512 + lane * 8; c < (uint32_t)d; c += (uint32_t)parts * 512) {   // unsigned: c passes d
     raw_t t8[ROWS], p8[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {   // a row that is not there is read as row 0 and not used
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const T* __restrict__ dx
       const int i = __ffsll((unsigned long long)left) - 1;
       left &= left - 1;
       float* to = G.grad + (k0 + i) * d;
-      for (int c = lane * 4; c < d; c += 256) store4(to + c, zero);
+      for (uint32_t c = lane * 4; c < (uint32_t)d; c += 256) store4(to + c, zero);
     }
     return;
   }
@@ -390,7 +390,7 @@ hipError_t embed_packed_fwd(int32_t dtype, const int32_t* ids, const void* tok, 
                             void* x, int64_t tokens, int32_t S, int32_t d, int32_t V, hipStream_t stream) {
   const PackedRows p{seq_start, n_seq, (int32_t)tokens};
   const int64_t pairs = (tokens + ROWS - 1) / ROWS;
-  const int parts = pairs < 2048 ? (d + 511) / 512 : 1;   // 2048 waves: two a SIMD
+  const int parts = pairs < 2048 ? (int)(((int64_t)d + 511) / 512) : 1;   // 2048 waves: two a SIMD
   const dim3 grid((unsigned)((pairs * parts + 3) / 4)), block(256);
   if (dtype == PF_DTYPE_BF16_)
     hipLaunchKernelGGL(embed_packed_kernel<bf16_t>, grid, block, 0, stream, ids, (const bf16_t*)tok, (const bf16_t*)pos, p, scale, (bf16_t*)x, S, d, V, parts);

@@ -54,7 +54,7 @@ int32_t launched(const char* who, hipError_t e) {
 }
 
 int32_t embed_args(const char* who, int32_t dtype, const int32_t* seq_start, int32_t n_seq, int64_t tokens, int32_t S, int32_t d, int32_t V) {
-  if (bad_dtype(dtype) || bad_sequences(seq_start, n_seq, tokens) || S <= 0 || d <= 0 || d % 8 != 0 || V <= 0 || tokens > (1 << 26) || tokens * ((d + 511) / 512) > (1 << 26) ||
+  if (bad_dtype(dtype) || bad_sequences(seq_start, n_seq, tokens) || S <= 0 || d <= 0 || d % 8 != 0 || V <= 0 || tokens > (1 << 26) || tokens * (((int64_t)d + 511) / 512) > (1 << 26) ||
       V > (1 << 24) || S > (1 << 24))
     return pf::fail(PF_ERR_ARG, "%s: bad argument (d must be a multiple of 8; at most 2^24 token ids and positions, tokens times d / 512 at most 2^26; seq_start NULL exactly when n_seq is 0)", who);
   return PF_OK;

@@ -174,3 +174,31 @@ def test_embedding_operands_aligned_to_16_bytes_and_no_more(dtype, d):
         results.append(got)
     assert all(torch.equal(a, b) for a, b in zip(*results))
     assert all(bool(t.any()) for t in results[0])
+
+
+def test_embedding_of_the_widest_rows():
+    """One row of 2^31 - 8 columns: a column's number and the next one's a wave goes on to pass 31 bits.  55 GB."""
+    pf, _ = _mods()
+    d, V, piece = 2 ** 31 - 8, 1, 1 << 26
+    if torch.cuda.mem_get_info()[0] < 70 << 30:
+        pytest.skip("needs 70 GB of free device memory")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    some = torch.randn(piece, device="cuda", generator=gen).to(torch.bfloat16)
+    tok, x = (torch.empty(V * d, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    for c in range(0, d, piece):
+        tok[c:c + piece] = some[:min(piece, d - c)]
+    x.fill_(7.0)
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pf.pf_op_embed_packed(pf.PF_DTYPE_BF16, ids.data_ptr(), tok.data_ptr(), None, None, 0, 1.0, x.data_ptr(), 1, 1, d, V)
+    torch.cuda.synchronize()
+    same = lambda a, f: all(torch.equal(a[c:c + piece], f(some[:min(piece, d - c)])) for c in range(0, d, piece))
+    assert same(x, lambda p: p)
+    del tok
+    dtok = torch.full((V * d,), 5.0, device="cuda")
+    n = pf.pf_op_embed_packed_bwd_workspace(1, 1, d, V)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for accumulate, id_, want in ((0, 0, lambda p: 2.0 * p.float()), (1, 0, lambda p: 4.0 * p.float()), (0, 5, lambda p: torch.zeros_like(p, dtype=torch.float32))):
+        ids.fill_(id_)       # 5: no row of the table, which becomes zeros
+        pf.pf_op_embed_packed_bwd(pf.PF_DTYPE_BF16, x.data_ptr(), ids.data_ptr(), None, 0, 2.0, dtok.data_ptr(), None, accumulate, ws.data_ptr(), n, 1, 1, d, V)
+        torch.cuda.synchronize()
+        assert same(dtok, want), (accumulate, id_)
