@@ -247,6 +247,20 @@ inline int heads_together(const PackedAttn& a) {
   return heads;
 }
 
+// How a bf16 call (d_head 64 / 128) is run, by its sizes alone: K/V tiles shared by the waves of a workgroup, a block's keys in one part or
+// two (d_head 128), or independent waves with 1, 2 or 4 to a block's keys; heads of a workgroup (shared tiles); whether all workgroups start at
+// the same time, so that blocks need no order.
+enum FwdForm : int32_t { SHARED_1, SHARED_2, WAVES_1, WAVES_2, WAVES_4 };
+struct FwdPlan {
+  FwdForm form;
+  int32_t heads, at_once;
+};
+FwdPlan packed_fwd_plan(const PackedAttn& a);
+struct BwdPlan {
+  int32_t splits, dkv_at_once, dq_at_once;   // splits: parts of a block's tiles in dK/dV
+};
+BwdPlan packed_bwd_plan(const PackedAttn& a);
+
 // bf16, d_head 64 / 128, all pointers 16-byte aligned, strides in eights
 hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st);
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,

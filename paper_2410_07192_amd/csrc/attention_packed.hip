@@ -531,6 +531,13 @@ hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* 
 #undef PF_FWD
 }
 
+int32_t attention_packed_route(const PackedAttn& a, bool aligned) {
+  if (!aligned || !aligned16(a, {}) || !by_bf16(a)) return splits_f32(a) << 16;
+  const FwdPlan f = packed_fwd_plan(a);
+  const BwdPlan b = packed_bwd_plan(a);
+  return (1 + f.form) | (f.at_once ? 0 : 1 << 8) | (b.dkv_at_once ? 0 : 1 << 9) | (b.dq_at_once ? 0 : 1 << 10) | f.heads << 12 | b.splits << 16;
+}
+
 int64_t packed_partial_bytes(const PackedAttn& a, int splits) { return splits > 1 ? (int64_t)splits * 2 * a.tokens * a.h_kv * a.dh * 4 : 0; }
 
 hipError_t packed_join(const PackedAttn& a, const float* partial, int splits, void* dk, void* dv, hipStream_t st) {

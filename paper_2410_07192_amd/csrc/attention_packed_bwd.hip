@@ -454,6 +454,11 @@ hipError_t run(const PackedAttn& a, const BwdArgs& b, hipStream_t st) {
 
 }  // namespace
 
+BwdPlan packed_bwd_plan(const PackedAttn& a) {
+  const BwdArgs b = plan_of(a);
+  return BwdPlan{b.splits, b.at_once & 1, (b.at_once >> 1) & 1};
+}
+
 int64_t packed_bwd_bf16_bytes(const PackedAttn& a) { return packed_partial_bytes(a, splits_of(a)); }
 
 hipError_t packed_bwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, const void* dout, const float* lse, const float* dsum, void* dq, void* dk,

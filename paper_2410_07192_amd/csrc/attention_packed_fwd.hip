@@ -394,24 +394,24 @@ __global__ __launch_bounds__(256, DH == 64 ? 2 : 1) void packed_fwd_units_kernel
 }
 
 template <int DH, int KG>
-hipError_t launch_units(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+hipError_t launch_units(const PackedAttn& a, const PackedQkv<bf16_t>& o, const FwdPlan& p, void* out, float* lse, hipStream_t st) {
   constexpr int lds = 4 * (2 * 64 * DH * 2 + 2048);
   hipError_t e = allow_lds((const void*)packed_fwd_units_kernel<DH, KG>, lds);
   if (e != hipSuccess) return e;
   const int64_t blocks = (a.tokens + 31) / 32, units = blocks * a.h;
-  hipLaunchKernelGGL((packed_fwd_units_kernel<DH, KG>), dim3((unsigned)((units * KG + 3) / 4)), dim3(256), lds, st, o, (bf16_t*)out, lse, (int32_t)blocks, units, units * KG / 4 <= (DH == 64 ? 512 : 256),
+  hipLaunchKernelGGL((packed_fwd_units_kernel<DH, KG>), dim3((unsigned)((units * KG + 3) / 4)), dim3(256), lds, st, o, (bf16_t*)out, lse, (int32_t)blocks, units, p.at_once,
                      LOG2E_P * o.scale);
   return hipGetLastError();
 }
 
 template <int DH, int KG>
-hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, int heads, void* out, float* lse, hipStream_t st) {
+hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, const FwdPlan& p, void* out, float* lse, hipStream_t st) {
   constexpr int lds = 2 * KG * 2 * 64 * DH * 2;
   hipError_t e = allow_lds((const void*)packed_fwd_bf16_kernel<DH, KG>, lds);
   if (e != hipSuccess) return e;
-  const int rows = 128 / heads, log_rows = __builtin_ctz(rows);
+  const int rows = 128 / p.heads, log_rows = __builtin_ctz(rows);
   const int64_t blocks = (a.tokens + rows - 1) / rows;
-  const FwdGrid grid{heads, a.h / heads, (int32_t)blocks, log_rows, blocks * (a.h / heads) * KG <= (DH == 64 ? 768 : 512), LOG2E_P * o.scale};
+  const FwdGrid grid{p.heads, a.h / p.heads, (int32_t)blocks, log_rows, p.at_once, LOG2E_P * o.scale};
   hipLaunchKernelGGL((packed_fwd_bf16_kernel<DH, KG>), dim3((unsigned)(blocks * grid.groups)), dim3(256 * KG), lds, st, o, (bf16_t*)out, lse, grid);
   return hipGetLastError();
 }
@@ -424,7 +424,6 @@ hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, int heads, vo
 // us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 14.9 / 13.9 / 15.8 / 12.1 / 10.0; 16 sequences up
 // to 2048 59 / 58 / 65 / 83 / 119; 2 up to 8192, 32 on 4 heads 868 / 977 / 1325 / 1415 / 1816; 12 heads of 64, 32 up to 512
 // 23.5 / - / 24.6 / 27.6 / 34.4.
-enum FwdForm { SHARED_1, SHARED_2, WAVES_1, WAVES_2, WAVES_4 };
 FwdForm fwd_form(const PackedAttn& a, int heads) {
   struct Cost { FwdForm form; int parts, slots; double start, full, alone; };
   static const Cost costs64[] = {{SHARED_1, 1, 768, 5.85, 2.14, 0.91}, {WAVES_1, 1, 512, 5.66, 1.61, 0.85}, {WAVES_2, 2, 512, 6.01, 1.43, 0.79},
@@ -454,16 +453,25 @@ FwdForm fwd_form(const PackedAttn& a, int heads) {
 
 }  // namespace
 
-hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+FwdPlan packed_fwd_plan(const PackedAttn& a) {
   const int heads = heads_together(a);
-  switch (fwd_form(a, heads)) {
-    case WAVES_1: return a.dh == 64 ? launch_units<64, 1>(a, o, out, lse, st) : launch_units<128, 1>(a, o, out, lse, st);
-    case WAVES_2: return a.dh == 64 ? launch_units<64, 2>(a, o, out, lse, st) : launch_units<128, 2>(a, o, out, lse, st);
-    case WAVES_4: return a.dh == 64 ? launch_units<64, 4>(a, o, out, lse, st) : launch_units<128, 4>(a, o, out, lse, st);
-    case SHARED_2:
-      if (a.dh == 128) return launch<128, 2>(a, o, heads, out, lse, st);
-      [[fallthrough]];
-    default: return a.dh == 64 ? launch<64, 1>(a, o, heads, out, lse, st) : launch<128, 1>(a, o, heads, out, lse, st);
+  const FwdForm form = fwd_form(a, heads);
+  const bool shared = form == SHARED_1 || form == SHARED_2, small = a.dh == 64;
+  const int parts = form == SHARED_2 || form == WAVES_2 ? 2 : form == WAVES_4 ? 4 : 1;
+  const int64_t rows = shared ? 128 / heads : 32;
+  const int64_t work = (a.tokens + rows - 1) / rows * (shared ? a.h / heads : a.h) * parts;   // shared: fours of waves; else waves
+  return FwdPlan{form, heads, shared ? work <= (small ? 768 : 512) : work / 4 <= (small ? 512 : 256)};
+}
+
+hipError_t packed_fwd_bf16(const PackedAttn& a, const PackedQkv<bf16_t>& o, void* out, float* lse, hipStream_t st) {
+  const FwdPlan p = packed_fwd_plan(a);
+  const bool small = a.dh == 64;
+  switch (p.form) {
+    case WAVES_1: return small ? launch_units<64, 1>(a, o, p, out, lse, st) : launch_units<128, 1>(a, o, p, out, lse, st);
+    case WAVES_2: return small ? launch_units<64, 2>(a, o, p, out, lse, st) : launch_units<128, 2>(a, o, p, out, lse, st);
+    case WAVES_4: return small ? launch_units<64, 4>(a, o, p, out, lse, st) : launch_units<128, 4>(a, o, p, out, lse, st);
+    case SHARED_2: return small ? hipErrorInvalidValue : launch<128, 2>(a, o, p, out, lse, st);   // there is none of d_head 64, and no rule picks it
+    default: return small ? launch<64, 1>(a, o, p, out, lse, st) : launch<128, 1>(a, o, p, out, lse, st);
   }
 }
 

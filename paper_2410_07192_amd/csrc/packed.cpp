@@ -100,6 +100,14 @@ int32_t pf_op_attention_packed_bwd(const pf_packed_attn* desc, const int32_t* se
   return launched("pf_op_attention_packed_bwd", pf::attention_packed_bwd(a, q, k, v, out, dout, lse, dq, dk, dv, workspace, (hipStream_t)stream));
 }
 
+// For tests: attention_packed_route of a call (misaligned: its pointers are not aligned to 16 bytes)
+int32_t pf_attention_packed_route(const pf_packed_attn* desc, int32_t misaligned) {
+  pf::PackedAttn a;
+  static const int32_t some = 0;
+  const int32_t rc = attention_args("pf_attention_packed_route", desc, desc && desc->n_seq > 0 ? &some : nullptr, &a);
+  return rc != PF_OK ? rc : pf::attention_packed_route(a, !misaligned);
+}
+
 int32_t pf_op_embed_packed(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, const int32_t* seq_start, int32_t n_seq, float scale, void* x,
                            int64_t tokens, int32_t S, int32_t d, int32_t V, void* stream) {
   const int32_t rc = embed_args("pf_op_embed_packed", dtype, seq_start, n_seq, tokens, S, d, V);

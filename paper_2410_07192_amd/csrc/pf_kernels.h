@@ -82,6 +82,10 @@ struct PackedAttn {
 hipError_t attention_packed_fwd(const PackedAttn& a, const void* q, const void* k, const void* v, void* out, float* lse,
                                 hipStream_t stream);
 int64_t attention_packed_bwd_bytes(const PackedAttn& a);   // of workspace
+// Which kernels a call takes (aligned: its pointers are, to 16 bytes).  Bits 0-7: forward, 0 fp32 products, else bf16 products in form
+// 1 + FwdForm (attention_packed.h).  Bits 8, 9, 10: blocks of the forward, of dK/dV and of dQ are taken longest first, as not all workgroups start
+// at once.  Bits 12-15: heads of a workgroup with shared tiles.  Bits 16-23: parts of a block's tiles in dK/dV.
+int32_t attention_packed_route(const PackedAttn& a, bool aligned);
 hipError_t attention_packed_bwd(const PackedAttn& a, const void* q, const void* k, const void* v, const void* out, const void* dout,
                                 const float* lse, void* dq, void* dk, void* dv, void* workspace, hipStream_t stream);
 hipError_t embed_packed_fwd(int32_t dtype, const int32_t* ids, const void* tok, const void* pos, const int32_t* seq_start,
