@@ -202,3 +202,81 @@ def test_embedding_of_the_widest_rows():
         pf.pf_op_embed_packed_bwd(pf.PF_DTYPE_BF16, x.data_ptr(), ids.data_ptr(), None, 0, 2.0, dtok.data_ptr(), None, accumulate, ws.data_ptr(), n, 1, 1, d, V)
         torch.cuda.synchronize()
         assert same(dtok, want), (accumulate, id_)
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 64), ("bf16", 32), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_operands_and_gradients_in_buffers_of_their_own(dtype, dh, causal):
+    """Q, K and V with a stride each, none of them the other's, no lse asked for: the same bits as from one fused buffer."""
+    pf, _ = _mods()
+    lens, h, kv = [90, 1, 140], 4, 2
+    c = Case(dtype, lens, h, kv, dh, causal, 2, 3, seed=11)
+    o, lse = c.forward()
+    want = c.backward(o, lse)
+    code = pf.PF_DTYPE_F32 if dtype == "f32" else pf.PF_DTYPE_BF16
+    lds = [h * dh, kv * dh + 8, kv * dh + 40, h * dh + 16]
+    desc = pf.packed_attn(code, c.T, len(lens), h, kv, dh, causal, 0, *lds[1:])     # 0: no gaps
+
+    def put(a, ld, fill=np.nan):
+        rows = np.full((c.T, ld), fill, np.float32)
+        rows[:, :a.shape[1] * dh] = a.reshape(c.T, -1)
+        return torch.from_numpy(rows).cuda().to(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+    q, k, v, do, out = (put(a, ld) for a, ld in ((c.q, lds[0]), (c.k, lds[1]), (c.v, lds[2]), (c.do, lds[3]), (o, lds[3])))
+    got = torch.full_like(out, 7.0)
+    pf.pf_op_attention_packed(desc, c.d_start.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), got.data_ptr())
+    d_lse = torch.from_numpy(lse).cuda()
+    grads = [torch.full_like(x, 7.0) for x in (q, k, v)]
+    n = pf.pf_op_attention_packed_bwd_workspace(desc)
+    ws = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")
+    pf.pf_op_attention_packed_bwd(desc, c.d_start.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), do.data_ptr(), d_lse.data_ptr(),
+                                  *(g.data_ptr() for g in grads), ws.data_ptr(), n)
+    torch.cuda.synchronize()
+    for x, w in zip([got] + grads, (o,) + want):
+        x, heads = x.float().cpu().numpy(), w.shape[1]
+        assert np.array_equal(x[c.live, :heads * dh], w.reshape(c.T, -1)[c.live])
+        assert (x[~c.live] == 7.0).all() and (x[:, heads * dh:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 64), ("bf16", 16), ("bf16", 64), ("bf16", 128)])
+def test_a_batch_of_empty_sequences(dtype, dh):
+    """Nothing is written: the checks of rows that no sequence holds are in forward and backward themselves."""
+    c = Case(dtype, [0, 0, 0], 4, 2, dh, True, 37, 20)
+    c.forward()
+    c.backward(np.zeros((c.T, 4, dh), np.float32), np.zeros((4, c.T), np.float32))
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 8), ("f32", 64), ("bf16", 32), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("n,h,kv", [(1, 65535, 1), (1, 65535, 13107), (5000, 4, 2), (70000, 1, 1)])
+def test_sequences_of_one_token_in_closed_form(dtype, dh, n, h, kv):
+    """The most heads, and more sequences than a wave looks at at once: out = v, lse = the row's score, dV = the sum of dO over the heads of a
+    group, dS = P (dP - D) = 0 up to the rounding of dP - D, at most (d_head + 2) 2^-24 sum |do| (|v| + |out|), and dQ, dK that times scale |k|, |q|."""
+    pf, _ = _mods()
+    tt, code = (torch.float32, pf.PF_DTYPE_F32) if dtype == "f32" else (torch.bfloat16, pf.PF_DTYPE_BF16)
+    gen = torch.Generator(device="cuda").manual_seed(n + h)
+    rnd = lambda heads: torch.randn(n, heads, dh, device="cuda", generator=gen).to(tt)
+    q, k, v, do = rnd(h), rnd(kv), rnd(kv), rnd(h)
+    start = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    desc = pf.packed_attn(code, n, n, h, kv, dh, True)
+    out, lse = torch.zeros_like(q), torch.zeros(h, n, device="cuda")
+    pf.pf_op_attention_packed(desc, start.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr())
+    dq, dk, dv = (torch.full_like(x, 7.0) for x in (q, k, v))
+    m = pf.pf_op_attention_packed_bwd_workspace(desc)
+    ws = torch.full((m,), 0xff, dtype=torch.uint8, device="cuda")
+    pf.pf_op_attention_packed_bwd(desc, start.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), do.data_ptr(), lse.data_ptr(), dq.data_ptr(),
+                                  dk.data_ptr(), dv.data_ptr(), ws.data_ptr(), m)
+    torch.cuda.synchronize()
+    g, u, scale = h // kv, 2.0 ** -24, dh ** -0.5
+    step = 2.0 ** -8 if dtype == "bf16" else u
+    by_head = lambda x: x.double().repeat_interleave(g, 1)
+    by_group = lambda x: x.view(n, kv, g, -1).sum(2)
+    assert torch.equal(out, v.repeat_interleave(g, 1))
+    s, mag = (q.double() * by_head(k)).sum(-1) * scale, (q.double() * by_head(k)).abs().sum(-1) * scale
+    assert ((lse.double().t() - s).abs() <= u * (dh + 4) * mag + 4 * u * s.abs()).all()
+    p = 1 + u * ((dh + 4) * mag + 16 + 4 * s.abs())               # P, exp of a rounding error
+    r = 2.0 ** -8 if dtype == "bf16" and dh >= 64 else 0.0       # P as an operand
+    sums = by_group(do.double().abs())
+    assert ((dv.double() - by_group(do.double())).abs() <= (r + u * (g + 32 + (dh + 4) * float(mag.max()) + 4 * float(s.abs().max()))) * sums + step * sums).all()
+    e = u * (dh + 2) * 2 * (do.double() * by_head(v)).abs().sum(-1, keepdim=True) * p[..., None] * 2
+    assert (dq.double().abs() <= e * scale * by_head(k).abs() * (1 + 2.0 ** -7) + 2.0 ** -95).all()
+    assert (dk.double().abs() <= by_group(e * scale * q.double().abs()) * (1 + 2.0 ** -7) + 2.0 ** -95).all()
