@@ -33,7 +33,11 @@ __device__ __forceinline__ Span queries_of(const PackedRows& p, int r0, int row,
 __device__ __forceinline__ int lane_value(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 // A lane's row sees rows lo .. hi - 1 of a tile of 64 (either may lie outside): all of the tile; a part of it, neither all nor nothing;
-// and whether row i is not among them (one comparison; length: hi - lo).  (Without short circuits: these are lane masks, not branches.)
+// and whether row i is not among them (one comparison; length: hi - lo).
+// Without short circuits, which can cost a result: `uniform && (lane test || lane test) ? a : -m` becomes a branch per lane into a block that a
+// wave-uniform branch enters too, and where the value that this block computes is free (a negation, an element of a vector), the compiler's
+// structurizer (ROCm 7.2) moves it to the block above and drops it for the lanes that come from the lane test; they keep a.  (In the compiler's
+// output right before that pass the value is there, right after it is not; a tile's keys were lost so.)  Masks with & and | are selects.
 __device__ __forceinline__ bool seen_as_a_whole(int lo, int hi) { return (lo <= 0) & (hi >= 64); }
 __device__ __forceinline__ bool seen_in_part(int lo, int hi) {
   const bool all = seen_as_a_whole(lo, hi), some = max(lo, 0) < min(hi, 64);

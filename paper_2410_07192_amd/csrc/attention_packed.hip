@@ -16,9 +16,11 @@
 //    that contracts over those rows; its "A" operand is a row of V (K, Q, dO) read as 32 consecutive columns.
 //  * A pair that is not visible has P = dS = 0, and 0 times an infinity or NaN of another sequence's row would be NaN: masked
 //    tiles with such a value take their sum row by row, visible ones only.
-// Large calls are bound by the fp32 matrix rate (two sequences of 2048, 16 heads of 64: forward 185 us, 93 of the 154 TFLOP/s that a large
-// product reaches; backward 841 us, 72 with the scores computed in both passes), small ones by one wave's chain over its tiles and the
-// launch (262 rows of four sequences, 4 heads of 64: 10 us; backward 20).
+// Large calls are bound by the fp32 matrix rate (two sequences of 2048, causal, 16 heads of 64: forward 187 us, 92 of the 154 TFLOP/s that a large
+// product reaches; backward 812 us, 74 with the scores computed in both passes), small ones by one wave's chain over its tiles and the
+// launch (262 rows of four sequences up to 128, 4 heads of 64: 11 us; causal backward, on 2 K/V heads, 25 to 27).
+// bf16 operands that the bf16 kernels do not take (8 sequences of 512, causal, 16 heads on 4, forward / backward): d_head 32 45 / 183 us, d_head 8
+// 29 / 90; rows at odd elements, d_head 64 95 / 373 (aligned: 17 / 49), d_head 128 193 / 1094 (23 / 84).
 #include "attention_packed.h"
 
 #include <algorithm>
@@ -143,13 +145,16 @@ __global__ __launch_bounds__(256) void packed_fwd_f32_kernel(PackedQkv<T> a, T* 
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) fv[dt][r] = col_of<DH>(vh, a.ld_v, min(k0 + reg_row(r, g), k_end - 1), dt, lr);
     const bool masked = k0 < in_lo || k0 + 31 >= in_hi;
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = k0 + reg_row(r, g);
+        if ((key < own.lo) | (key >= own.hi)) s[r] = -INFINITY;
+      }
+    }
     float mx = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int key = k0 + reg_row(r, g);
-      if (masked && (key < own.lo || key >= own.hi)) s[r] = -INFINITY;
-      mx = fmaxf(mx, s[r]);
-    }
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
     const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, 64)));
     const float ref = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = __expf(m - ref);   // no reference point yet: exp(-inf) = 0
@@ -302,7 +307,7 @@ __device__ __forceinline__ void dkv_f32_block(const BwdF32<T>& b, int unit, floa
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int q = q0 + reg_row(r, g);   // L and D of row q are in lane q - q0
-      const bool hidden = masked && (q < own.lo || q >= own.hi);
+      const bool hidden = masked & hidden_at(q, own.lo, own.hi - own.lo);
       const float Lq = __shfl(L, reg_row(r, g), 64), Dq = __shfl(D, reg_row(r, g), 64);
       const float p = hidden ? 0.f : __expf(s[r] - Lq);
       dp[r] = hidden ? 0.f : p * (dp[r] - Dq);
@@ -388,10 +393,11 @@ __device__ __forceinline__ void dq_f32_block(const BwdF32<T>& b, int unit, float
     }
     const bool masked = k0 < in_lo || k0 + 31 >= in_hi;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int key = k0 + reg_row(r, g);
-      const bool hidden = masked && (key < own.lo || key >= own.hi);
-      dp[r] = hidden ? 0.f : __expf(s[r] - L) * (dp[r] - D);
+    for (int r = 0; r < 16; ++r) dp[r] = __expf(s[r] - L) * (dp[r] - D);
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (hidden_at(k0 + reg_row(r, g), own.lo, own.hi - own.lo)) dp[r] = 0.f;
     }
     float xt[DT][16];
 #pragma unroll
@@ -483,7 +489,7 @@ hipError_t fwd(const PackedAttn& a, const void* q, const void* k, const void* v,
 }
 // Splits of a block's tiles in dK/dV: as many as fill the card, four tiles (one a wave) to each or more if sequences were all as long as
 // they are on average.  (us in one launch, and with one split and a launch for each pass: 262 rows, 4 heads on 2 of 64, one sequence
-// 22, 65 (three splits), four 20, 36 (one); 512 rows, 4 heads of 128 45, 100 (three); 4096 rows, 16 heads of 64 841, 914 (one).)
+// 22, 65 (three splits), four of 32 to 100 rows 20, 36 (one); 512 rows, causal, 4 heads of 128 43, 100 (three); two of 2048, 16 heads of 64 812, 914 (one).)
 int splits_f32(const PackedAttn& a) {
   const int64_t units = (a.tokens + 31) / 32 * a.h_kv, length = a.tokens / (a.n_seq > 1 ? a.n_seq : 1);
   const int64_t tiles = ((a.causal ? length / 2 : length) + 63) / 32 * (a.h / a.h_kv);

@@ -280,3 +280,20 @@ def test_sequences_of_one_token_in_closed_form(dtype, dh, n, h, kv):
     e = u * (dh + 2) * 2 * (do.double() * by_head(v)).abs().sum(-1, keepdim=True) * p[..., None] * 2
     assert (dq.double().abs() <= e * scale * by_head(k).abs() * (1 + 2.0 ** -7) + 2.0 ** -95).all()
     assert (dk.double().abs() <= by_group(e * scale * q.double().abs()) * (1 + 2.0 ** -7) + 2.0 ** -95).all()
+
+
+@pytest.mark.parametrize("dtype,lens,h,kv,dh,shift", ODD, ids=name)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("score", [np.inf, np.nan])
+def test_a_score_of_infinity_or_nan(dtype, lens, h, kv, dh, shift, causal, score):
+    """The rows that see it have no softmax: NaN in out and lse.  Rows before it (causal) and other sequences' have theirs."""
+    def edit(c):
+        c.q[:, :, 3] = 1
+        c.k[c.start[0:-1:2] + AT, :, 3] = score
+
+    c = Case(dtype, lens, h, kv, dh, causal, 3, 2, shift=shift, seed=12, edit=edit)
+    o, lse = c.forward()
+    for s, (a, b) in enumerate(zip(c.start[:-1], c.start[1:])):
+        first = b if s % 2 else a + AT if causal else a
+        assert np.isnan(o[first:b]).all() and np.isnan(lse[:, first:b]).all()
+        assert np.isfinite(o[a:first]).all() and np.isfinite(lse[:, a:first]).all()
