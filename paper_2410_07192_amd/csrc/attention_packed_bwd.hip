@@ -12,8 +12,9 @@
 //  * dQ: the forward kernel's mirror image; S^T = K Q^T and dP^T = V dO^T put one query into a lane.
 // Tiles go global -> LDS directly, one tile ahead.  Bound by what a SIMD issues: matrix products, exponentials and LDS reads take about as
 // long each (seven products of 2 T^2 d_head per head and pass where the formulas have five: S and dP in both passes), and two waves
-// overlap them in part.  d_head 64, 16 heads on 4, one sequence of 8192: 494 us, 0.97 PFLOP/s of products; d_head 128: see below.
-// D = rowsum(dO O) comes from a launch before (5 us at 5000 rows of 16 heads of 64).  Rows of other sequences: see attention_packed.h.  A workgroup whose results
+// overlap them in part.  d_head 64, 16 heads on 4, one causal sequence of 8192: 480 to 500 us, 0.96 to
+// 1.0 PFLOP/s of products; d_head 128: 1000 to 1050, see below.
+// D = rowsum(dO O) comes from a launch before (6 us at 5000 rows of 16 heads of 64).  Rows of other sequences: see attention_packed.h.  A workgroup whose results
 // hold an infinity or NaN, which rows hidden from them may have brought in, does them again with care, as a second stretch of code behind the first
 // (woven into the first it cost that one registers: dK/dV of d_head 128 took 1880 us instead of 780).
 #include "attention_packed.h"
@@ -175,7 +176,7 @@ __device__ __forceinline__ bool dkv_block(const BwdArgs& a, int unit, char* smem
       f32x16 aS, aP;
 #pragma unroll
       for (int r = 0; r < 16; ++r) aS[r] = aP[r] = 0.f;
-      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(1);   // the SIMD's other wave fills the gaps (1081 -> 1023 us at 8192 rows, 16 heads on 4; d_head 64: 483 -> 501)
+      if constexpr (DH == 128) __builtin_amdgcn_s_setprio(1);   // the SIMD's other wave fills the gaps (side by side, 8192 rows, 16 heads on 4: 1081 -> 1023 us; d_head 64: 483 -> 501)
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const int r = qs * 32 + lr;
@@ -372,8 +373,8 @@ __device__ __forceinline__ bool dq_block(const BwdArgs& a, int unit, char* smem,
 
 // Both passes in one launch, the dK/dV workgroups first, they are the longer ones.  d_head 128: dK and dV come from workgroups of their own
 // (PAIR), which compute the scores twice but have half the sums each, so that two waves fit a SIMD and one's matrix products run beside the
-// other's exponentials (8 sequences of 1024, 16 heads on 4: 199 us, 241 with both in one workgroup; 20 of 300, 16 heads: 139, 186; d_head 64
-// has room for both: 8192 rows 483 us so, 594 apart at three waves a SIMD).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
+// other's exponentials (side by side, 8 sequences of 1024, 16 heads on 4: 199 us, 241 with both in one workgroup; 20 of 300, 16 heads: 139, 186;
+// d_head 64 has room for both: 8192 rows 483 us so, 594 apart at three waves a SIMD).  The two of a unit are eight apart: on the same XCD, with the same Q and dO in its L2.
 template <int DH, bool CAREFUL>
 __device__ __forceinline__ bool block(const BwdArgs& a, int unit, char* smem, int* s_span) {
   constexpr bool PAIR = DH == 128;
@@ -403,11 +404,11 @@ double rows_met(const PackedAttn& a) {
   return a.causal ? length / 2 : length;
 }
 
-// Parts of a block's tiles in dK/dV: the number with the least estimated time.  A workgroup takes `start` and `tile` us per tile of 64
+// Parts of a block's tiles in dK/dV: the number with the least cost, which ranks them and is no time.  A workgroup takes `start` and `tile` per tile of 64
 // queries; either the card's `slots` are full, or the longest block's chain counts (its sequence `longest` times the average);
-// with parts, their fp32 sums go through memory at 4 TB/s in `join` us more.  Fitted to 350 sizes with 1 to 16 parts (MI355X):
-// 3 % off the best number on average, 33 % at most (one part everywhere: 37 %).  us with 1 / 2 / 4 / 8 / 16 parts: 16 heads of 128
-// on 2, 8114 rows of 2 sequences 1172 / 692 / 591 / 610 / 669; 16 of 64 on 4, 4680 rows of 8: 207 / 119 / 84 / 101 / 130.
+// with parts, their fp32 sums go through memory at 4 TB/s in `join` more.  Fitted to 350 sizes with 1 to 16 parts (MI355X):
+// 3 % off the best number on average, 33 % at most (one part everywhere: 37 %).  us with 1 / 2 / 4 / 8 / 16 parts, causal: 16 heads of 128
+// on 2, 2 sequences of 4057 1100 / 666 / 568 / 583 / 652 (the rule: 4); 16 of 64 on 4, 8 of 585 83 / 59 / 60 / 76 / 107 (3: 55).
 int splits_of(const PackedAttn& a) {
   struct Cost { double start, tile, slots, join, longest; };
   const Cost c = a.dh == 64 ? Cost{3.07, 1.2, 207, 2.37, 1.93} : Cost{13.2, 1.55, 155, 2.63, 1.83};

@@ -10,8 +10,8 @@
 // More heads and fewer rows read the same K/V for the same products but end nearer to the causal diagonal and to the ends of sequences.
 //
 // Bound by what a SIMD issues: for a wave's tile of d_head 128, matrix products take 1024 cycles, its share of the CU's LDS reads as many
-// and the softmax about 900, and two waves overlap them in part: two sequences up to 8192, 32 heads on 4 of 128: 860 us, 1.04 PFLOP/s
-// (a large bf16 product reaches 1.2); scores one tile ahead of their softmax in program order made it 838 from 805 us at 14192 rows, because
+// and the softmax about 900, and two waves overlap them in part: two sequences up to 8192, 32 heads on 4 of 128: 836 to 880 us, 1.02 to 1.07
+// PFLOP/s (a large bf16 product reaches 1.2), the matrix units busy half of the cycles at 1.8 GHz; scores one tile ahead of their softmax in program order made it 838 from 805 us at 14192 rows, because
 // the products then issue together all the same.  Short calls are bound by a block's chain: launch, boundaries, Q, first tiles, about 5 us
 // before the first product, then 0.8 to 1.3 us a tile.
 #include "attention_packed.h"
@@ -169,7 +169,8 @@ struct FwdGrid {
 };
 // A workgroup's block of rows and heads: four waves share K/V tiles.  KG = 2: twice four, the second four with every other tile, so
 // that a block's own chain over the keys is half as long; their sums meet in LDS.
-// Registers for three waves a SIMD (d_head 64; 12 sequences of 1024, 16 heads on 4: 46.6 us, 53.0 with two; four do not fit, 108) or two.
+// Registers for three waves a SIMD (d_head 64; 12 sequences of 1024, 16 heads on 4, side by side: 46.6 us, 53.0 with two; four do not fit, 108; now
+// 42.2) or two.
 template <int DH, int KG>
 __global__ __launch_bounds__(256 * KG, DH == 64 ? 3 : 2) void packed_fwd_bf16_kernel(PackedQkv<bf16_t> a, bf16_t* __restrict__ out, float* __restrict__ lse, FwdGrid grid) {
   constexpr int NW = 4, TILE = 64 * DH * 2, BUF = KG * 2 * TILE, DT = DH / 32, LD = DH + 4;
@@ -416,14 +417,15 @@ hipError_t launch(const PackedAttn& a, const PackedQkv<bf16_t>& o, const FwdPlan
   return hipGetLastError();
 }
 
-// Which form is fastest: shared tiles, a block's keys in one or two parts, or independent waves with 1, 2 or 4 to a unit's keys.  The
-// estimate of each is the longer of two times and some of the other: its workgroups go through the card (start + tiles x full us, times
-// the number of fillings of its `slots`), and its longest block's chain (start + tiles x alone us).  Lengths are on the device, so the
-// longest sequence is taken to be twice the average.  The constants are fitted to 600 sizes timed in every form (MI355X): 2.0 % (d_head 64)
+// Which form is fastest: shared tiles, a block's keys in one or two parts, or independent waves with 1, 2 or 4 to a unit's keys.  Each
+// form's cost is the longer of two terms and some of the other: its workgroups go through the card (start + tiles x full, times
+// the number of fillings of its `slots`), and its longest block's chain (start + tiles x alone).  Lengths are on the device, so the
+// longest sequence is taken to be twice the average.  The costs rank the forms and are no times: 16 prompts up to 2048 are put at 36 and
+// take 52 us, 2 documents up to 8192 at 1591 and take 874.  Their constants are fitted to 600 sizes timed in every form (MI355X): 2.0 % (d_head 64)
 // and 1.6 % (128) off the fastest form on average, 47 % at most; the best single form would be 16 % and 26 % off.
-// us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 14.9 / 13.9 / 15.8 / 12.1 / 10.0; 16 sequences up
-// to 2048 59 / 58 / 65 / 83 / 119; 2 up to 8192, 32 on 4 heads 868 / 977 / 1325 / 1415 / 1816; 12 heads of 64, 32 up to 512
-// 23.5 / - / 24.6 / 27.6 / 34.4.
+// us in forms shared 1 / shared 2 / waves 1 / 2 / 4: 16 heads on 2 of 128, 333 rows 13.3 / 13.3 / 14.2 / 11.0 / 8.9; 16 sequences up
+// to 2048 51.8 / 54.3 / 58.0 / 74.8 / 114; 2 up to 8192, 32 on 4 heads 874 / 960 / 1199 / 1331 / 1890; 12 heads of 64, 32 up to 512
+// 21.1 / - / 23.7 / 24.4 / 30.0 (the rule takes one wave, 12 % off).
 FwdForm fwd_form(const PackedAttn& a, int heads) {
   struct Cost { FwdForm form; int parts, slots; double start, full, alone; };
   static const Cost costs64[] = {{SHARED_1, 1, 768, 5.85, 2.14, 0.91}, {WAVES_1, 1, 512, 5.66, 1.61, 0.85}, {WAVES_2, 2, 512, 6.01, 1.43, 0.79},

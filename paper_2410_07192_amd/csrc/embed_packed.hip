@@ -2,7 +2,7 @@
 //
 // Forward: x[t] = scale tok[ids[t]] + pos[t - start(t)], one rounding.  Bound by HBM: a wave takes two rows, 16 bytes a lane, with
 // all their loads in flight at once (14500 rows of 2048, bf16: 20.7 us with all columns to a wave, 4.1 TB/s; one row a wave 21.5, four
-// 24.2, eight 28.0).  Few rows cannot hide the four loads one after the other (sequence, id, table, store) behind each other, so each
+// 24.2, eight 28.0; fp32 47).  Few rows cannot hide the four loads one after the other (sequence, id, table, store) behind each other, so each
 // wave takes one slice of 512 columns then (266 rows of 1816: 8.2 us, 12.0 with all columns).
 //
 // Backward: dtok[v] = scale sum over rows t with ids[t] = v of dx[t], dpos[p] = sum over rows at position p of dx[t], fp32, in
@@ -17,8 +17,9 @@
 //      group inside a wave's share goes to its gradient row at once, the sums of groups that go beyond to the workspace.
 //      Other waves clear the rest of the rows that no row of dx belongs to.
 //   3. embed_join_kernel adds those partial sums up in order.
-// Large tables are bound by writing the gradient (7250 rows of 1024, bf16, into 50257 rows: 54 us for 206 MB of it and 15 MB of dx read
-// twice), small ones by the three launches after each other (549 rows of 512, fp32, into 10007: 5.4 + 7.8 + 3.9).
+// Large tables are bound by writing the gradient (7250 rows of 1024, bf16, into 50257 rows: 55 us, 42 with nothing else in between, for 206 MB of it
+// and 15 MB of dx read twice; added to what is there, without clearing, 30), small ones by the three launches after each other (553 rows of 512,
+// fp32, into 10007: 5.6 + 7.0 + 3.9).
 #include "packed.h"
 #include "pf_device.h"
 #include "pf_kernels.h"
@@ -359,7 +360,7 @@ BwdLayout bwd_layout(int64_t tokens, int64_t S, int64_t d, int64_t V) {
   L.own = (int32_t)((V + ((int64_t)1 << L.log_wgs) - 1) >> L.log_wgs);
   L.slices = (int32_t)((d + 511) / 512);
   // Entries per wave.  Eight are loaded at a time, so few waves are done earlier with eight each, many carry fewer partial sums and read
-  // less about their groups with 16 (549 rows of 512, fp32: 18.6 us with 16, 16.8 with 8; 4000 of 680: 18.9, 17.8; 7250 of 1024:
+  // less about their groups with 16 (553 rows of 512, fp32: 18.6 us with 16, 16.8 with 8; 4000 of 680: 18.9, 17.8; 7250 of 1024:
   // 45.4, 48.4; 12400 of 400: 27.5, 28.7).  Positions have as many waves as tokens.
   L.share = (tokens + 15) / 16 * L.slices * 2 < 1280 ? 8 : 16;
   L.shares = (tokens + L.share - 1) / L.share;

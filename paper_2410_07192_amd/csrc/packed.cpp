@@ -35,7 +35,7 @@ int32_t attention_args(const char* who, const pf_packed_attn* d, const int32_t* 
   if (a->ld_q < wq || a->ld_k < wk || a->ld_v < wk || a->ld_out < wq || std::max(std::max(a->ld_q, a->ld_k), std::max(a->ld_v, a->ld_out)) > MAX_STRIDE)
     return pf::fail(PF_ERR_ARG, "%s: bad argument (rows overlap, or a stride over 2^24)", who);
   if ((d->tokens + 31) / 32 * d->n_heads > MAX_BLOCKS)
-    return pf::fail(PF_ERR_ARG, "%s: bad argument (tokens * n_heads is more than 2^27)", who);
+    return pf::fail(PF_ERR_ARG, "%s: bad argument (ceil(tokens / 32) * n_heads is more than 2^22)", who);
   a->tokens = d->tokens;
   a->seq_start = seq_start;
   a->n_seq = d->n_seq;
